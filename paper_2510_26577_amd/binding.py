@@ -20,6 +20,8 @@ SRC_PATH = os.path.join(_HERE, "csrc", "tva.hip")
 CAST_SRC_PATH = os.path.join(_HERE, "csrc", "cast.cpp")  # host part: tree-size selection
 VERIFY_SRC_PATH = os.path.join(_HERE, "csrc", "verify.hip")  # acceptance + commit kernels
 DRAFT_SRC_PATH = os.path.join(_HERE, "csrc", "draft.hip")    # draft-tree expansion + subtree kernels
+CACHE4_SRC_PATH = os.path.join(_HERE, "csrc", "cache4.hip")  # 4-bit rows: store, load, attention
+EVICT_SRC_PATH = os.path.join(_HERE, "csrc", "evict.hip")    # key weights, choice of slots, moves
 PYCALL_SRC_PATH = os.path.join(_HERE, "csrc", "pycall.cpp")  # calls on tensors in native code (module _pycall)
 PYCALL_LIB_PATH = os.path.join(_HERE, "_pycall.so")
 INCLUDE_DIR = os.path.join(_ROOT, "include")
@@ -43,13 +45,13 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17",
 
 
 def build_library(verbose: bool = False, timeline: bool = False) -> str:
-    """Compile csrc/tva.hip, csrc/verify.hip and csrc/draft.hip (gfx950 kernels + their C ABI) and csrc/cast.cpp
-    (host logic) into libtva.so (in-tree); timeline=True: the instrumented build libtva_timeline.so
+    """Compile csrc/tva.hip, csrc/verify.hip, csrc/draft.hip, csrc/cache4.hip and csrc/evict.hip (gfx950 kernels + their
+    C ABI) and csrc/cast.cpp (host logic) into libtva.so (in-tree); timeline=True: the instrumented build libtva_timeline.so
     (paper_2510_26577_amd/timeline.py) instead."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out = TIMELINE_LIB_PATH if timeline else LIB_PATH
     cmd = [hipcc, *HIPCC_FLAGS, *(["-DTVA_TIMELINE"] if timeline else []), "-I", INCLUDE_DIR, "-shared", "-fPIC", "-o", out,
-           SRC_PATH, VERIFY_SRC_PATH, DRAFT_SRC_PATH, CAST_SRC_PATH]
+           SRC_PATH, VERIFY_SRC_PATH, DRAFT_SRC_PATH, CACHE4_SRC_PATH, EVICT_SRC_PATH, CAST_SRC_PATH]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     lines = [l for l in res.stdout.splitlines() if "is not a recognized feature" not in l]
     if verbose or res.returncode:
@@ -111,6 +113,10 @@ DRAFT_EXPORTS = ("tva_expand_workspace_bytes", "tva_expand_layer", "tva_sizeof_e
                  "tva_layer_breadth_count")
 VERIFY_EXPORTS = ("tva_accept_greedy", "tva_accept_greedy_filled", "tva_accept_sampling", "tva_accept_sampling_filled", "tva_accept_sampling_wait_bound_test", "tva_sample_workspace_bytes", "tva_sample_workspace_bytes_rows", "tva_sizeof_sample_args", "tva_commit_path",
                   "tva_sizeof_commit_args")
+# entry points of include/tva_cache.h (bound in cache4.py and evict.py)
+CACHE_EXPORTS = ("tva_cache_store", "tva_cache_load", "tva_sizeof_rows_args", "tva_tree_verify_attn_4bit", "tva_attn4_workspace_bytes",
+                 "tva_attn4_plan_splits", "tva_sizeof_attn4_args", "tva_key_weights", "tva_sizeof_key_weight_args", "tva_evict_select",
+                 "tva_sizeof_evict_select_args", "tva_evict_move", "tva_sizeof_evict_move_args")
 # host entry points of include/tva_cast.h (bound in cast.py)
 CAST_EXPORTS = ("tva_cast_select_context", "tva_cast_select_max_valid_index", "tva_cast_layer_utility",
                 "tva_cast_layer_cost", "tva_cast_breadth_prune", "tva_cast_depth_bytes", "tva_cast_depth_init",
@@ -194,14 +200,18 @@ def _bind_native(lib) -> None:
         raise RuntimeError(f"{PYCALL_LIB_PATH} not built: run `python -c 'import __graft_entry__ as g; g.build()'`")
     from . import _pycall
     at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
-    for name in ("tva_sizeof_sample_args", "tva_sizeof_commit_args", "tva_sizeof_expand_args"):
+    for name in ("tva_sizeof_sample_args", "tva_sizeof_commit_args", "tva_sizeof_expand_args", *(n for n in CACHE_EXPORTS if "sizeof" in n)):
         getattr(lib, name).restype = ctypes.c_size_t
     sizes = lib.tva_sizeof_args() + 1024 * (lib.tva_sizeof_sample_args() + 1024 * lib.tva_sizeof_commit_args())
     if _pycall.sizes != sizes or _pycall.functions != len(_NATIVE_CALLS):
         raise RuntimeError("_pycall.so is stale: rebuild it")
     _pycall.bind(*map(at, _NATIVE_CALLS))
     for size, names in ((lib.tva_sizeof_args(), ("tva_tree_verify_attn", "tva_tree_verify_attn_static", "tva_tree_verify_attn_splits")),
-                        (lib.tva_sizeof_expand_args(), ("tva_expand_layer",)), (lib.tva_sizeof_commit_args(), ("tva_commit_path",))):
+                        (lib.tva_sizeof_expand_args(), ("tva_expand_layer",)), (lib.tva_sizeof_commit_args(), ("tva_commit_path",)),
+                        (lib.tva_sizeof_rows_args(), ("tva_cache_store", "tva_cache_load")),
+                        (lib.tva_sizeof_attn4_args(), ("tva_tree_verify_attn_4bit",)),
+                        (lib.tva_sizeof_key_weight_args(), ("tva_key_weights",)),
+                        (lib.tva_sizeof_evict_select_args(), ("tva_evict_select",)), (lib.tva_sizeof_evict_move_args(), ("tva_evict_move",))):
         for name in names:
             _address[name] = (at(name), size)
     _native = _pycall

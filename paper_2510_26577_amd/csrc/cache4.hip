@@ -1,0 +1,666 @@
+// libtva: caches of 4-bit rows (gfx950).  Entry points and formats: include/tva_cache.h.
+//
+//   store_rows_kernel  bf16 rows -> 4-bit rows: 8 elements per lane, D/8 lanes per row; the largest magnitudes (of 32
+//                      elements for K, of the row for V) are integer maxima of bf16 bits over neighbouring lanes.
+//   load_rows_kernel   the inverse.
+//   four_bit_kernel    the verification attention: S^T = K Q^T and O^T = V^T P^T by 32x32x16 bf16 MFMAs, as in
+//                      tva.hip, on tiles of 64 keys that every wave streams for itself.  A tile is 8.6 KB (D = 128), a
+//                      quarter of a bf16 one, so that the next one waits in registers: K's bytes are the
+//                      operand's own lanes' (a lane's key, half of the elements) and are widened there; V's pass
+//                      through 4 KB of LDS that belong to the wave, because the transposing read (16 x 16 codes per 16
+//                      lanes) wants rows.  No barrier in the loop.
+//   join_kernel        merges the KV splits' partial results.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_rows.h"
+#include "tva.h"
+#include "tva_cache.h"
+
+namespace {
+
+using namespace cache_rows;
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// ---------------------------------------------------------------------------------------
+// rows in, rows out
+// ---------------------------------------------------------------------------------------
+struct RowsParams {
+  const int32_t *cu_T, *L, *path, *path_len;
+  uint16_t *k_rows, *v_rows;
+  CacheView c;
+  int32_t *L_out, *err_flag;
+  int Hkv, max_rows;
+  int64_t layer_rows;   // elements of k_rows / v_rows between layers
+  int64_t layer_cache;  // rows of the cache between layers
+};
+
+// The row of k_rows / v_rows and the cache row of (sequence, j, head): false if there is none.
+__device__ __forceinline__ bool find_row(const RowsParams &p, int b, int j, int g, int64_t *from, int64_t *to) {
+  const int t0 = p.cu_T[b], T = p.cu_T[b + 1] - t0;
+  int n = p.path ? p.path_len[b] : T;
+  if (j >= (n < p.max_rows ? n : p.max_rows)) return false;
+  const int node = p.path ? p.path[(int64_t)b * p.max_rows + j] : j;
+  const int64_t pos = (int64_t)p.L[b] + j;
+  if (node < 0 || node >= T || pos < 0 || pos >= room_of(p.c, b)) {
+    if (p.err_flag && g == 0) atomicCAS(p.err_flag, 0, 1 + b);
+    return false;
+  }
+  *from = (int64_t)t0 + node;
+  *to = position_at(p.c, b, (int)pos) + g * p.c.stride_head;
+  return true;
+}
+
+// |x| bits of the largest finite of eight bf16 numbers
+__device__ __forceinline__ uint32_t largest(const u16x8 x) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t m = x[i] & 0x7fff;
+    a = m < 0x7f80 && m > a ? m : a;
+  }
+  return a;
+}
+// Code of x / s: s times the borders between codes is exact (s has at most 4 significant bits, a border 3), and so are the
+// comparisons.  NaN compares false: 0.
+__device__ __forceinline__ uint32_t code_of(float x, float s) {
+  const float a = fabsf(x);
+  const uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) + (a >= 3.5f * s) + (a > 5.f * s);
+  return c | (a == a ? (__float_as_uint(x) >> 28) & 8u : 0u);
+}
+__device__ __forceinline__ uint32_t codes_of(const u16x8 x, float s) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= code_of(__uint_as_float((uint32_t)x[i] << 16), s) << (4 * i);
+  return w;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) store_rows_kernel(const RowsParams p) {
+  constexpr int LPR = D / 8;  // lanes per row
+  const int b = blockIdx.y, layer = blockIdx.z;
+  const int idx = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, part = threadIdx.x % LPR;
+  const int j = idx / p.Hkv, g = idx - j * p.Hkv;
+  if (idx == 0 && part == 0 && layer == 0 && p.L_out) {
+    const int n = p.path ? p.path_len[b] : p.cu_T[b + 1] - p.cu_T[b];
+    p.L_out[b] = p.L[b] + (n < p.max_rows ? n : p.max_rows);
+  }
+  int64_t from, to;
+  if (!find_row(p, b, j, g, &from, &to)) return;  // (the lanes of a row leave together)
+  to += layer * p.layer_cache;
+  const int64_t e = layer * p.layer_rows + (from * p.Hkv + g) * D + part * 8;
+  const u16x8 k = *(const u16x8 *)(p.k_rows + e), v = *(const u16x8 *)(p.v_rows + e);
+  uint32_t ak = largest(k), av = largest(v);
+#pragma unroll
+  for (int o = 1; o < LPR; o *= 2) {
+    if (o < 4) ak = max(ak, (uint32_t)__shfl_xor((int)ak, o));
+    av = max(av, (uint32_t)__shfl_xor((int)av, o));
+  }
+  // K: a = (1 + m/128) 2^(E-127) <= 6 * 2^e
+  const int ek = min(max((int)(ak >> 7) - 127 - ((ak & 127) > 64 ? 1 : 2), -96), 124);
+  // V: a = n/256 * 2^(E-126), the quotient by 6 rounded up to four bits
+  const int n = 128 + (int)(av & 127), ev = (int)(av >> 7) - 126;
+  const float sv = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), ev - 7) : ldexpf((float)((n + 23) / 24), ev - 6), 0x1p-96f), 0x1p124f);
+  ((uint32_t *)p.c.k)[to * LPR + part] = codes_of(k, exponent_byte((uint32_t)(ek + 127)));
+  ((uint32_t *)p.c.v)[to * LPR + part] = codes_of(v, sv);
+  if (part % 4 == 0) ((uint8_t *)p.c.k_row_scale)[to * (D / 32) + part / 4] = (uint8_t)(ek + 127);
+  if (part == 0) ((uint16_t *)p.c.v_row_scale)[to] = (uint16_t)(__float_as_uint(sv) >> 16);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) load_rows_kernel(const RowsParams p) {
+  constexpr int LPR = D / 8;
+  const int b = blockIdx.y, layer = blockIdx.z;
+  const int idx = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, part = threadIdx.x % LPR;
+  const int j = idx / p.Hkv, g = idx - j * p.Hkv;
+  int64_t to, from;
+  if (!find_row(p, b, j, g, &to, &from)) return;
+  from += layer * p.layer_cache;
+  const int64_t e = layer * p.layer_rows + (to * p.Hkv + g) * D + part * 8;
+  const uint32_t k = ((const uint32_t *)p.c.k)[from * LPR + part], v = ((const uint32_t *)p.c.v)[from * LPR + part];
+  const float sk = exponent_byte(((const uint8_t *)p.c.k_row_scale)[from * (D / 32) + part / 4]);
+  const float sv = __uint_as_float((uint32_t)((const uint16_t *)p.c.v_row_scale)[from] << 16);
+  *(bf16x8 *)(p.k_rows + e) = widen8(k, sk);
+  bf16x8 x = widen8(v, 1.f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (__bf16)((float)x[i] * sv);  // (at most 6 bits: exact)
+  *(bf16x8 *)(p.v_rows + e) = x;
+}
+
+// ---------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------
+struct FourParams {
+  const __bf16 *q, *k_tree, *v_tree;
+  const int32_t *cu_T, *L, *parent;
+  const uint64_t *mask;
+  CacheView c;
+  __bf16 *out;
+  float *lse;
+  float *part_out, *part_lse;  // [S, sum_T * Hq, D], [S, sum_T * Hq] when S > 1
+  int Hq, Hkv, G, W, sum_T, max_L, S, chunk;  // chunk: keys per split, a multiple of 64
+  float scale_log2;
+};
+
+__device__ __forceinline__ float half_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+constexpr int kWaves = 4;
+
+// A node's V may hold what is not finite, and rows that do not see the node must not (0 * inf is NaN): such elements are taken out of
+// the operand, and rows that give them weight get their infinities from products of their own (NaN counts as both).
+__device__ __forceinline__ void add_infinite(bf16x8 &v, const bf16x8 w, f32x16 &acc) {
+  uint16_t x[8];
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+    any |= (x[i] & 0x7f80) == 0x7f80;
+  }
+  if (!__any(any)) return;
+  bf16x8 up, down;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool out = (x[i] & 0x7f80) == 0x7f80, nan = out && (x[i] & 0x7f);
+    up[i] = (__bf16)(out && (nan || x[i] == 0x7f80) ? 1.f : 0.f);
+    down[i] = (__bf16)(out && (nan || x[i] == 0xff80) ? 1.f : 0.f);
+    v[i] = out ? (__bf16)0.f : v[i];
+  }
+  f32x16 zero = {};
+  const f32x16 a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, w, zero, 0, 0, 0), b = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, w, zero, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = (acc[i] + (a[i] > 0.f ? INFINITY : 0.f)) - (b[i] > 0.f ? INFINITY : 0.f);
+}
+
+template <int D>
+struct FourCfg {
+  static constexpr int NS = D / 16;          // QK steps of 16 elements
+  static constexpr int NJ = D / 32;          // 32-wide blocks of the output
+  static constexpr int RB = D / 2;           // bytes of a row
+  static constexpr int CH = RB / 16;         // 16-byte pieces of a row = wave-wide loads of a V tile
+  static constexpr int RPL = 64 / CH;        // rows such a load covers
+  static constexpr int KL = RB / 32;         // 16-byte pieces of a lane's half of a K row
+  static constexpr int VT = 64 * RB;         // V tile
+  static constexpr int WAVE_LDS = VT + 256;  // V tile and its 64 scales
+  static constexpr int TP = D + 4;           // floats between rows of an output patch
+  static constexpr int PATCH = 32 * TP * 4;
+  static constexpr int EXCHANGE = 2 * kWaves * 32 * 4;  // maxima and sums
+  static constexpr int TREE = TVA_MAX_TREE * 4;
+  static constexpr int LOOP_LDS = kWaves * WAVE_LDS + TREE;
+  static constexpr int END_LDS = kWaves * PATCH + EXCHANGE;
+  static constexpr int LDS = LOOP_LDS > END_LDS ? LOOP_LDS : END_LDS;
+};
+
+// Grid: KV head (fastest: with 8 heads one per XCD), block of WM * 32 query rows, (sequence, split).  The four waves are
+// WM row groups x 4 / WM key groups; tile i of the split belongs to key group i % (4 / WM).
+template <int D, int WM, bool PAGED>
+__global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
+  typedef FourCfg<D> C;
+  constexpr int WK = kWaves / WM;
+  __shared__ __align__(16) unsigned char lds[C::LDS];
+  const int g = blockIdx.x, b = blockIdx.z / p.S, split = blockIdx.z - b * p.S;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wm = wave % WM, wk = wave / WM;
+  const int t0 = p.cu_T[b], T = min(p.cu_T[b + 1] - t0, TVA_MAX_TREE);
+  const int n_rows = T * p.G;
+  const int row0 = blockIdx.y * (WM * 32);
+  if (row0 >= n_rows) return;
+  const int L = min(max(p.L[b], 0), p.max_L);
+  const int last_split = L > 0 ? (L - 1) / p.chunk : 0;
+  const int key0 = split * p.chunk;
+  const int n_keys = split <= last_split ? min(p.chunk, L - key0) : 0;
+  const bool has_tree = split == last_split;
+  const int n_cache = (n_keys + 63) >> 6, n_tiles = n_cache + (has_tree ? (T + 63) >> 6 : 0);
+
+  // this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written
+  const int row = min(row0 + wm * 32 + l32, n_rows - 1);
+  const int node = row / p.G, head = g * p.G + (row - node * p.G);
+  const bool idle = row0 + wm * 32 >= n_rows;
+
+  f32x16 acc[C::NJ];
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+  float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
+
+  if (n_tiles > 0 && split <= last_split) {
+    // ancestor set of this lane's node, trimmed to the tree
+    uint64_t anc0 = 0, anc1 = 0;
+    if (has_tree) {
+      if (p.mask) {
+        const uint64_t *w = p.mask + (int64_t)(t0 + node) * p.W;
+        anc0 = w[0];
+        if (p.W > 1) anc1 = w[1];
+      } else {
+        int32_t *par = (int32_t *)(lds + kWaves * C::WAVE_LDS);
+        if (tid < T && tid < TVA_MAX_TREE) par[tid] = p.parent[t0 + tid];
+        __syncthreads();
+        int a = min(node, TVA_MAX_TREE - 1);
+        for (int step = 0; step < TVA_MAX_TREE; ++step) {
+          if (a < 64) anc0 |= 1ull << a;
+          else anc1 |= 1ull << (a - 64);
+          const int up = par[a];
+          if (up < 0 || up >= a) break;
+          a = up;
+        }
+      }
+      if (T < 64) anc0 &= (1ull << T) - 1, anc1 = 0;
+      else if (T < 128) anc1 &= (1ull << (T - 64)) - 1;
+    }
+
+    bf16x8 q[C::NS];
+    const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(qrow + s * 8);
+
+    unsigned char *vt = lds + wave * C::WAVE_LDS;
+    float *vsl = (float *)(vt + C::VT);
+
+    // ---- what waits in registers: K and V bytes of a tile and their scales ----
+    u32x4 kx[2][C::KL], vx[C::CH];
+    uint32_t ks[2];
+    uint16_t vs;
+    const int64_t head_rows = g * p.c.stride_head;
+    const int64_t dense0 = PAGED ? 0 : (int64_t)p.c.cu_L[b] * p.c.stride_tok + head_rows;
+    // row numbers of the tile's keys: K's (this lane's key in each block of 32), V's (the rows its loads cover), and key `lane`
+    auto row_of = [&](int key) __attribute__((always_inline)) -> int64_t {
+      const int t = key0 + min(key, n_keys - 1);  // rows past the end repeat the last one and are masked
+      if constexpr (PAGED) return position_at(p.c, b, t) + head_rows;
+      else return dense0 + (int64_t)t * p.c.stride_tok;
+    };
+    auto fetch = [&](int tile) __attribute__((always_inline)) {
+      int64_t rk[2], rv[C::CH], rs;
+      if constexpr (PAGED) {  // one table entry per key, handed out among the lanes
+        rs = row_of(tile * 64 + lane);
+        const int lo = (int)rs, hi = (int)(rs >> 32);
+        auto of = [&](int l) __attribute__((always_inline)) { return ((int64_t)__shfl(hi, l) << 32) | (uint32_t)__shfl(lo, l); };
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) rk[kb] = of(kb * 32 + l32);
+#pragma unroll
+        for (int i = 0; i < C::CH; ++i) rv[i] = of(i * C::RPL + lane / C::CH);
+      } else {
+        rs = row_of(tile * 64 + lane);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) rk[kb] = row_of(tile * 64 + kb * 32 + l32);
+#pragma unroll
+        for (int i = 0; i < C::CH; ++i) rv[i] = row_of(tile * 64 + i * C::RPL + lane / C::CH);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int i = 0; i < C::KL; ++i) kx[kb][i] = *(const u32x4 *)(p.c.k + rk[kb] * C::RB + half * (C::RB / 2) + i * 16);
+        if constexpr (D == 128) ks[kb] = *(const uint16_t *)(p.c.k_row_scale + rk[kb] * 4 + half * 2);
+        else ks[kb] = *(const uint8_t *)(p.c.k_row_scale + rk[kb] * 2 + half);
+      }
+#pragma unroll
+      for (int i = 0; i < C::CH; ++i) vx[i] = *(const u32x4 *)(p.c.v + rv[i] * C::RB + (lane % C::CH) * 16);
+      vs = *(const uint16_t *)(p.c.v_row_scale + rs * 2);
+    };
+
+    f32x16 s[2];
+    // scores -> probabilities in place (log2 domain, fp32), O and l moved to a new reference where a row's maximum grew
+    auto soften = [&]() __attribute__((always_inline)) {
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+      top = half_max(top) * p.scale_log2;
+      // the reference moves only when it is exceeded by more than 2^8: probabilities stay below that
+      if (__any(top > m + 8.f)) {
+        const float to = fmaxf(m, top);
+        const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+        m = to, l *= f;
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[j][i] *= f;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, -ref));
+          l += s[kb][i];
+        }
+    };
+
+    if (!idle) {
+      int tile = wk;
+      if (tile < n_cache) fetch(tile);
+      for (; tile < n_cache; tile += WK) {
+        // ---- V to LDS: piece c of row r lies at piece c ^ (r / 8) of its row, so that the 16 rows a transposing read takes
+        // together (4 consecutive ones of each 8) are in different banks
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < C::CH; ++i) {
+          const int r = i * C::RPL + lane / C::CH;
+          *(u32x4 *)(vt + r * C::RB + (((lane % C::CH) ^ (r >> 3)) & (C::CH - 1)) * 16) = vx[i];
+        }
+        vsl[lane] = __uint_as_float((uint32_t)vs << 16);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // ---- S^T = K Q^T
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < C::NS; ++st)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            const float sc = exponent_byte(st < C::NS / 2 || D == 64 ? ks[kb] & 255 : ks[kb] >> 8);
+            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(kx[kb][st / 4][st % 4], sc), q[st], s[kb], 0, 0, 0);
+          }
+        const int left = n_keys - tile * 64;
+        if (tile + WK < n_cache) fetch(tile + WK);
+        if (left < 64) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (kb * 32 + 8 * (i / 4) + 4 * half + i % 4 >= left) s[kb][i] = -INFINITY;
+        }
+        soften();
+        // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          bf16x8 w[2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 sc = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * half);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[i / 2][(i % 2) * 4 + k] = (__bf16)(s[kb][i * 4 + k] * sc[k]);
+          }
+          // this lane's row of the 16 x 16 codes its 16 lanes turn over: key slot i of its half, 8 bytes of elements
+          const int i16 = lane & 15, r = kb * 32 + 8 * (i16 >> 2) + 4 * half + (i16 & 3), sub = (lane >> 4) & 1;
+#pragma unroll
+          for (int j = 0; j < C::NJ; ++j) {
+            const i32x2 c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                (__attribute__((address_space(3))) i32x2 *)(vt + r * C::RB + ((j ^ (r >> 3)) & (C::CH - 1)) * 16 + sub * 8));
+#pragma unroll
+            for (int a = 0; a < 2; ++a) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)c[a], 1.f), w[a], acc[j], 0, 0, 0);
+          }
+        }
+      }
+      // ---- the tree's own keys, bf16
+      for (; tile < n_tiles; tile += WK) {
+        const int first = (tile - n_cache) * 64, left = T - first;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+          const int key = first + kb * 32 + l32;
+          const __bf16 *krow = p.k_tree + ((int64_t)(t0 + min(key, T - 1)) * p.Hkv + g) * D + half * (D / 2);
+          if (kb * 32 < left) {
+#pragma unroll
+            for (int st = 0; st < C::NS; ++st)
+              s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(krow + st * 8), q[st], s[kb], 0, 0, 0);
+          }
+          const uint64_t word = first ? anc1 : anc0;
+          const uint32_t bits = (uint32_t)(word >> (kb * 32));
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!((bits >> (8 * (i / 4) + 4 * half + i % 4)) & 1)) s[kb][i] = -INFINITY;
+        }
+        soften();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            if (kb * 32 + a * 16 >= left) continue;
+            bf16x8 w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[kb][a * 8 + i];
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j) {
+              bf16x8 v;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int key = first + kb * 32 + a * 16 + 8 * (i / 4) + 4 * half + i % 4;
+                v[i] = p.v_tree[((int64_t)(t0 + min(key, T - 1)) * p.Hkv + g) * D + j * 32 + l32];
+              }
+              add_infinite(v, w, acc[j]);
+              acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
+            }
+          }
+      }
+    }
+  }
+
+  // ---- the key groups' results joined, and O^T turned over to rows ----
+  l = half_sum(l);
+  __syncthreads();
+  float *patch = (float *)lds, *maxima = (float *)(lds + kWaves * C::PATCH), *sums = maxima + kWaves * 32;
+  if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < WK; ++k) top = fmaxf(top, maxima[(k * WM + wm) * 32 + l32]);
+  float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 x;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = acc[j][i * 4 + k] * f;
+      *(f32x4 *)(patch + wave * (32 * C::TP) + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
+    }
+  __syncthreads();
+  constexpr int PIECES = WM * 32 * (D / 4);
+  for (int x = tid; x < PIECES; x += 256) {
+    const int r = x / (D / 4), d = (x - r * (D / 4)) * 4, w = r >> 5, rr = r & 31;
+    if (row0 + r >= n_rows) break;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float top_r = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < WK; ++k) top_r = fmaxf(top_r, maxima[(k * WM + w) * 32 + rr]);
+#pragma unroll
+    for (int k = 0; k < WK; ++k) {
+      const int at = k * WM + w;
+      o += *(const f32x4 *)(patch + at * (32 * C::TP) + rr * C::TP + d);
+      const float mk = maxima[at * 32 + rr];
+      sum += mk == -INFINITY ? sums[at * 32 + rr] : sums[at * 32 + rr] * __builtin_amdgcn_exp2f(mk - top_r);  // (0, or NaN)
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
+    o *= inv;
+    const int rnode = (row0 + r) / p.G, rhead = g * p.G + (row0 + r - rnode * p.G);
+    const int64_t at = (int64_t)(t0 + rnode) * p.Hq + rhead;
+    const float lse = sum == 0.f ? -INFINITY : (top_r + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
+    if (p.S > 1) {
+      const int64_t n = (int64_t)p.sum_T * p.Hq;
+      if (sum != 0.f) *(f32x4 *)(p.part_out + ((int64_t)split * n + at) * D + d) = o;
+      if (d == 0) p.part_lse[(int64_t)split * n + at] = lse;
+    } else {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = (__bf16)o[k];
+      *(bf16x4 *)(p.out + at * D + d) = y;
+      if (d == 0 && p.lse) p.lse[at] = lse;
+    }
+  }
+}
+
+// Splits of one row per D/4 lanes: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(const float *part_out, const float *part_lse, int S, int64_t n, __bf16 *out, float *lse) {
+  constexpr int LPR = D / 4;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int d = (threadIdx.x % LPR) * 4;
+  if (row >= n) return;
+  float top = -INFINITY;
+  for (int s = 0; s < S; ++s) top = fmaxf(top, part_lse[s * n + row]);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  for (int s = 0; s < S; ++s) {
+    const float ls = part_lse[s * n + row];
+    if (ls == -INFINITY) continue;  // (nothing was written there)
+    const float w = __builtin_amdgcn_exp2f((ls - top) * kLog2e);
+    sum += w;
+    o += *(const f32x4 *)(part_out + (s * n + row) * D + d) * w;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  bf16x4 y;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) y[k] = (__bf16)(o[k] * inv);
+  *(bf16x4 *)(out + row * D + d) = y;
+  if (d == 0 && lse) lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+}
+
+struct FourPlan {
+  int WM, blocks, S, chunk;
+};
+bool plan_four(const tva_attn4_args *a, FourPlan *pl) {
+  const int G = a->Hq / a->Hkv;
+  const int64_t rows = (int64_t)a->max_T * G;
+  const int groups = (int)((rows + 31) / 32);
+  pl->WM = groups >= 3 ? 4 : groups == 2 ? 2 : 1;
+  pl->blocks = (int)((rows + pl->WM * 32 - 1) / (pl->WM * 32));
+  const int tiles = std::max(1, (a->max_L + 63) / 64);
+  const int64_t base = std::max<int64_t>(1, (int64_t)a->B * a->Hkv * pl->blocks);
+  int64_t S = a->num_splits;
+  if (S == 0) {
+    S = (512 + base - 1) / base;                            // two workgroups per CU
+    S = std::min<int64_t>(S, std::max(1, tiles * pl->WM / kWaves));  // a tile per wave
+  }
+  S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
+  const int per = (int)((tiles + S - 1) / S);
+  pl->chunk = per * 64;
+  pl->S = (tiles + per - 1) / per;
+  return true;
+}
+
+int check_four(const tva_attn4_args *a, bool shapes_only) {
+  if (!a || a->B <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv) return TVA_INVALID_ARG;
+  if (a->sum_T < 0 || a->max_T < 0 || a->max_L < 0 || a->num_splits < 0) return TVA_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (a->max_T > TVA_MAX_TREE) return TVA_UNSUPPORTED;
+  if (a->max_L > 0x7fffff00) return TVA_UNSUPPORTED;  // (positions are rounded up to whole tiles)
+  if (shapes_only) return TVA_OK;
+  if (!(a->scale > 0.f)) return TVA_INVALID_ARG;
+  if (a->sum_T == 0) return TVA_OK;
+  if (!a->cu_T || !a->L || !a->q || !a->k_tree || !a->v_tree || !a->out || (!a->anc_mask && !a->parent)) return TVA_INVALID_ARG;
+  if (((uintptr_t)a->q | (uintptr_t)a->k_tree | (uintptr_t)a->v_tree | (uintptr_t)a->out) & 15) return TVA_INVALID_ARG;
+  if (a->anc_mask && (a->mask_words < 1 || a->mask_words > 2 || a->mask_words * 64 < a->max_T)) return TVA_UNSUPPORTED;
+  if (a->cache.kind != TVA_ROWS_E2M1) return TVA_UNSUPPORTED;
+  return TVA_OK;
+}
+
+size_t four_bytes(const tva_attn4_args *a, const FourPlan &pl) {
+  return pl.S <= 1 ? 0 : (size_t)pl.S * a->sum_T * a->Hq * (a->D + 1) * 4;
+}
+
+template <int D>
+int launch_rows(const RowsParams &p, int B, int layers, bool load, hipStream_t st) {
+  const int64_t groups = ((int64_t)p.max_rows * p.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8));
+  if (groups > 0x7fffffff) return TVA_UNSUPPORTED;
+  const dim3 grid((unsigned)groups, B, layers);
+  if (load) hipLaunchKernelGGL(load_rows_kernel<D>, grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL(store_rows_kernel<D>, grid, dim3(256), 0, st, p);
+  return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
+}
+
+int run_rows(const tva_rows_args *a, bool load, void *stream) {
+  if (!a || a->B < 0 || a->Hkv < 1 || a->max_rows < 0 || a->n_layers < 0) return TVA_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (a->B == 0) return TVA_OK;
+  if (a->cache.kind != TVA_ROWS_E2M1) return a->cache.kind < 0 || a->cache.kind > TVA_ROWS_E2M1 ? TVA_INVALID_ARG : TVA_UNSUPPORTED;
+  if (!a->cu_T || !a->L || (a->path == nullptr) != (a->path_len == nullptr)) return TVA_INVALID_ARG;
+  if (!a->k_rows || !a->v_rows || (((uintptr_t)a->k_rows | (uintptr_t)a->v_rows) & 15)) return TVA_INVALID_ARG;
+  if (a->L_out && (a->L_out == a->L || load)) return TVA_INVALID_ARG;
+  if (a->layer_stride_cache < 0 || a->layer_stride_rows < 0 || a->layer_stride_cache % a->D || a->layer_stride_rows % 8) return TVA_INVALID_ARG;
+  const int layers = a->n_layers > 0 ? a->n_layers : 1;
+  if (a->B > 65535 || layers > 65535) return TVA_UNSUPPORTED;
+  RowsParams p{};
+  const int rc = view_of(a->cache, a->Hkv, a->D, true, &p.c);
+  if (rc != TVA_OK) return rc;
+  if (a->max_rows == 0) return TVA_OK;
+  p.cu_T = a->cu_T, p.L = a->L, p.path = a->path, p.path_len = a->path_len;
+  p.k_rows = (uint16_t *)a->k_rows, p.v_rows = (uint16_t *)a->v_rows;
+  p.L_out = a->L_out, p.err_flag = a->err_flag, p.Hkv = a->Hkv, p.max_rows = a->max_rows;
+  p.layer_rows = a->layer_stride_rows, p.layer_cache = a->layer_stride_cache / a->D;
+  (void)hipGetLastError();
+  return a->D == 128 ? launch_rows<128>(p, a->B, layers, load, (hipStream_t)stream) : launch_rows<64>(p, a->B, layers, load, (hipStream_t)stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tva_cache_store(const tva_rows_args *a, void *stream) { return run_rows(a, false, stream); }
+int tva_cache_load(const tva_rows_args *a, void *stream) { return run_rows(a, true, stream); }
+size_t tva_sizeof_rows_args(void) { return sizeof(tva_rows_args); }
+
+size_t tva_attn4_workspace_bytes(const tva_attn4_args *a) {
+  FourPlan pl;
+  if (check_four(a, true) != TVA_OK || !plan_four(a, &pl)) return (size_t)-1;
+  return four_bytes(a, pl);
+}
+
+int32_t tva_attn4_plan_splits(const tva_attn4_args *a) {
+  FourPlan pl;
+  if (check_four(a, true) != TVA_OK || !plan_four(a, &pl)) return -1;
+  return pl.S;
+}
+
+int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream) {
+  int rc = check_four(a, false);
+  if (rc != TVA_OK) return rc;
+  if (a->sum_T == 0 || a->max_T == 0) return TVA_OK;
+  FourPlan pl;
+  FourParams p{};
+  rc = view_of(a->cache, a->Hkv, a->D, true, &p.c);
+  if (rc != TVA_OK) return rc;
+  plan_four(a, &pl);
+  const size_t need = four_bytes(a, pl);
+  if (need && (!a->workspace || ((uintptr_t)a->workspace & 15))) return TVA_INVALID_ARG;
+  if (a->workspace_bytes < need) return TVA_WORKSPACE_TOO_SMALL;
+  if ((int64_t)a->B * pl.S > 65535 || pl.blocks > 65535) return TVA_UNSUPPORTED;
+  p.q = (const __bf16 *)a->q, p.k_tree = (const __bf16 *)a->k_tree, p.v_tree = (const __bf16 *)a->v_tree;
+  p.cu_T = a->cu_T, p.L = a->L, p.parent = a->parent, p.mask = a->anc_mask;
+  p.out = (__bf16 *)a->out, p.lse = a->lse;
+  const int64_t n = (int64_t)a->sum_T * a->Hq;
+  p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (pl.S > 1 ? pl.S * n * a->D : 0);
+  p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.sum_T = a->sum_T, p.max_L = a->max_L;
+  p.S = pl.S, p.chunk = pl.chunk, p.scale_log2 = a->scale * kLog2e;
+  const dim3 grid(a->Hkv, pl.blocks, a->B * pl.S);
+  const hipStream_t st = (hipStream_t)stream;
+  const bool paged = a->cache.page_table != nullptr;
+  (void)hipGetLastError();
+  auto launch = [&](auto d, auto wm) {
+    constexpr int D = decltype(d)::value, WM = decltype(wm)::value;
+    if (paged) hipLaunchKernelGGL((four_bit_kernel<D, WM, true>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((four_bit_kernel<D, WM, false>), grid, dim3(256), 0, st, p);
+    if (pl.S > 1 && hipPeekAtLastError() == hipSuccess)
+      hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)((n + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, p.part_out, p.part_lse, pl.S, n, p.out, p.lse);
+  };
+  auto shapes = [&](auto d) {
+    if (pl.WM == 1) launch(d, std::integral_constant<int, 1>{});
+    else if (pl.WM == 2) launch(d, std::integral_constant<int, 2>{});
+    else launch(d, std::integral_constant<int, 4>{});
+  };
+  if (a->D == 128) shapes(std::integral_constant<int, 128>{});
+  else shapes(std::integral_constant<int, 64>{});
+  return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
+}
+
+size_t tva_sizeof_attn4_args(void) { return sizeof(tva_attn4_args); }
+
+}  // extern "C"

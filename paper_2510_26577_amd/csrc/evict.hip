@@ -1,0 +1,488 @@
+// libtva: eviction from K/V caches (gfx950).  Entry points and their meaning: include/tva_cache.h.
+//
+//   weigh_kernel   attention weights of cached keys, summed over a step's accepted rows.  S = Q K^T by 32x32x16 bf16 MFMAs with a
+//                  key per lane: a wave holds the operands of its keys and streams row blocks past them, so that K is read once
+//                  and a key's sum stays in its lane.  No atomics: a key has one wave.
+//   choose_kernel  which slots of a weight row stay: one workgroup per row.  The n-th largest key is found digit by digit (8 bits,
+//                  histograms in LDS), the kept set is then a bit per slot, and gaps and fillers are matched by rank.
+//   shift_kernel   the rows that fill the gaps: sources and destinations are disjoint, so every row moves by itself.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_rows.h"
+#include "tva.h"
+#include "tva_cache.h"
+
+namespace {
+
+using namespace cache_rows;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------------------------------
+// weights of keys
+// ---------------------------------------------------------------------------------------
+struct WeighParams {
+  const int32_t *cu_T, *path, *path_len, *L, *first_pos;
+  const __bf16 *q;
+  const float *lse;
+  CacheView c;
+  float *weight;
+  int32_t *pos;
+  int64_t ld;
+  int Hq, Hkv, G, max_rows, max_L;
+  float scale_log2;
+};
+
+__device__ __forceinline__ float half_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Four consecutive E4M3 bytes' pairs -> bf16 (exact)
+__device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+constexpr int kWeighWaves = 4;
+
+// Grid: KV head, 128 * KB keys, sequence.  Wave w has keys 32 KB w .. 32 KB (w + 1) - 1 of the workgroup's.
+template <int D, int KIND, int KB>
+__global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighParams p) {
+  constexpr int NS = D / 16;
+  __shared__ __align__(16) float lds[kWeighWaves][2][32];
+  const int g = blockIdx.x, b = blockIdx.z;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int t0 = p.cu_T[b], T = p.cu_T[b + 1] - t0;
+  const int all = p.L[b], L = min(all, p.max_L);
+  const int n = min(min(p.path ? p.path_len[b] : T, p.max_rows), all);
+  const int key0 = (blockIdx.y * kWeighWaves + wave) * (32 * KB);
+  if (n <= 0 || key0 >= L) return;  // (no barriers below: a wave keeps to itself)
+
+  // ---- this lane's keys as operands: elements 16 s + 8 half of step s (bf16), or half of the row per lane half
+  bf16x8 k[KB][NS];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int64_t at = position_at(p.c, b, min(key0 + kb * 32 + l32, L - 1)) + g * p.c.stride_head;
+    if constexpr (KIND == TVA_ROWS_BF16) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[kb][s] = *(const bf16x8 *)(p.c.k + (at + s * 16 + half * 8) * 2);
+    } else if constexpr (KIND == TVA_ROWS_E4M3) {
+      u32x4 x[NS / 2];
+#pragma unroll
+      for (int s = 0; s < NS / 2; ++s) x[s] = *(const u32x4 *)(p.c.k + at + half * (D / 2) + s * 16);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[kb][s] = widen8_e4m3(u32x2{x[s / 2][s % 2 * 2], x[s / 2][s % 2 * 2 + 1]});
+    } else {
+      u32x4 x[NS / 4];
+#pragma unroll
+      for (int s = 0; s < NS / 4; ++s) x[s] = *(const u32x4 *)(p.c.k + at * (D / 2) + half * (D / 4) + s * 16);
+      uint32_t sc;
+      if constexpr (D == 128) sc = *(const uint16_t *)(p.c.k_row_scale + at * 4 + half * 2);
+      else sc = *(const uint8_t *)(p.c.k_row_scale + at * 2 + half);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[kb][s] = widen8(x[s / 4][s % 4], exponent_byte(s < 4 ? sc & 255 : sc >> 8));
+    }
+  }
+
+  float sum[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) sum[kb] = 0.f;
+  const int old = all - n;  // positions below it are seen by every row
+  const bool all_seen = key0 + 32 * KB <= old;
+  const int R = n * p.G;
+  float *lrow = lds[wave][0];
+  int *seen_to = (int *)lds[wave][1];
+  for (int r0 = 0; r0 < R; r0 += 32) {
+    // rows r0 .. r0+31: query operand (a row per lane), log-sum-exp and last seen position
+    const int r = min(r0 + l32, R - 1), i = r / p.G, head = g * p.G + (r - i * p.G);
+    const int node = p.path ? p.path[(int64_t)b * p.max_rows + i] : i;
+    const bool there = node >= 0 && node < T;
+    const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
+    const float lse = p.lse[row];
+    const bool counts = there && r0 + l32 < R && lse != -INFINITY;
+    bf16x8 q[NS];
+    const __bf16 *from = p.q + row * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      q[s] = *(const bf16x8 *)(from + (KIND == TVA_ROWS_BF16 ? s * 16 + half * 8 : half * (D / 2) + s * 8));
+      if (!counts) q[s] = bf16x8{};  // (whatever it holds)
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (half == 0) lrow[l32] = counts ? -lse * kLog2e : -INFINITY, seen_to[l32] = old + i;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    f32x16 x[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) x[kb] = f32x16{};
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[kb][s], x[kb], 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const f32x4 l = *(const f32x4 *)(lrow + 8 * c + 4 * half);
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      i32x4 to = {};
+      if (!all_seen) to = *(const i32x4 *)(seen_to + 8 * c + 4 * half);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[kb][c * 4 + e], p.scale_log2, l[e]));
+          sum[kb] += all_seen || key0 + kb * 32 + l32 <= to[e] ? w : 0.f;
+        }
+    }
+  }
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const float w = half_sum(sum[kb]);
+    const int t = key0 + kb * 32 + l32;
+    const int64_t at = ((int64_t)b * p.Hkv + g) * p.ld + t;
+    if (half || t >= L) continue;
+    p.weight[at] = (t < old ? p.weight[at] : 0.f) + w;
+    if (p.pos && t >= old) p.pos[at] = p.first_pos[b] + (t - old);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// which slots stay
+// ---------------------------------------------------------------------------------------
+struct ChooseParams {
+  const int32_t *L, *keep, *newest, *pos;
+  const float *weight;
+  int32_t *src, *L_out;
+  int64_t ld, ld_src;
+  int B, H, max_L, n_first, words;  // words: 64-slot words of the longest row
+};
+
+constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kCopies = 16;
+
+// Slots in the order they are kept: larger first.  Protected above everything, NaN below, -0 as 0.
+__device__ __forceinline__ uint32_t key_of(const ChooseParams &p, float w, bool safe) {
+  if (safe) return 0xffffffffu;
+  if (w != w) return 0;
+  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+
+__device__ __forceinline__ int ones(uint64_t x) { return (int)__popcll(x); }
+// The r-th set bit of w (r < popcount)
+__device__ __forceinline__ int select_bit(uint64_t w, int r) {
+  int at = 0;
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) {
+    const int c = ones(w & ((1ull << s) - 1));
+    if (r >= c) r -= c, w >>= s, at += s;
+  }
+  return at;
+}
+
+// Inclusive sum over the workgroup's threads, and its total
+__device__ __forceinline__ int scan_threads(int x, int *part, int *total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // (part may still be read)
+  if (lane == 63) part[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kChooseWaves; ++w) {
+    before += w < wave ? part[w] : 0;
+    all += part[w];
+  }
+  *total = all;
+  return x + before;
+}
+
+// ITEMS > 0: the row's keys stay in registers (L <= 1024 * ITEMS); 0: they are read again in every pass.
+template <int ITEMS>
+__global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseParams p) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  uint64_t *above = (uint64_t *)lds, *equal = above + p.words;  // a bit per slot; above becomes the kept set
+  int *before = (int *)(equal + p.words);                        // gaps before each word
+  int *hist = before + p.words;                                  // [256][kCopies]
+  int *part = hist + 256 * kCopies;                              // 16, and 4 words of the search
+  const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int L = min(max(p.L[b], 0), p.max_L), n = (int)min((int64_t)min(max(p.keep[b], 0), L), p.ld_src);
+  if (h == 0 && layer == 0 && tid == 0 && p.L_out) p.L_out[b] = n;
+  const int64_t r = ((int64_t)layer * p.B + b) * p.H + h;
+  const float *weight = p.weight + r * p.ld;
+  const int32_t *pos = p.pos ? p.pos + r * p.ld : nullptr;
+  int32_t *src = p.src + r * p.ld_src;
+  if (n == L) {
+    for (int j = tid; j < n; j += kChooseThreads) src[j] = j;
+    return;
+  }
+  if (n == 0) return;
+  const int newest = p.newest ? p.newest[b] : 0x7fffffff;
+  const bool ages = p.newest != nullptr;
+  auto key_at = [&](int t) __attribute__((always_inline)) {
+    const int age = pos ? pos[t] : t;
+    return key_of(p, weight[t], t < p.n_first || (ages && age >= newest));
+  };
+  uint32_t keys[ITEMS > 0 ? ITEMS : 1];
+  if constexpr (ITEMS > 0) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int t = i * kChooseThreads + tid;
+      keys[i] = t < L ? key_at(t) : 0;
+    }
+  }
+  const int rounds = (L + kChooseThreads - 1) / kChooseThreads;
+  auto each = [&](auto use) __attribute__((always_inline)) {
+    if constexpr (ITEMS > 0) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+        if (i < rounds) use(i * kChooseThreads + tid, keys[i]);
+    } else {
+      for (int i = 0; i < rounds; ++i) {
+        const int t = i * kChooseThreads + tid;
+        use(t, t < L ? key_at(t) : 0u);
+      }
+    }
+  };
+
+  // ---- the n-th largest key: eight bits at a time, from the top
+  uint32_t prefix = 0;
+  int want = n;  // of the keys that begin with prefix, the want-th largest
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256 * kCopies; i += kChooseThreads) hist[i] = 0;
+    __syncthreads();
+    each([&](int t, uint32_t k) __attribute__((always_inline)) {
+      if (t < L && (shift == 24 || (k ^ prefix) >> (shift + 8) == 0)) atomicAdd(&hist[((k >> shift) & 255) * kCopies + (lane & (kCopies - 1))], 1);
+    });
+    __syncthreads();
+    int mine = 0;
+    const int digit = 255 - tid;  // thread 0 has the largest
+    if (tid < 256)
+      for (int c = 0; c < kCopies; ++c) mine += hist[digit * kCopies + c];
+    int total;
+    const int upto = scan_threads(mine, part, &total);
+    if (tid < 256 && upto >= want && upto - mine < want) part[16] = digit, part[17] = want - (upto - mine);
+    __syncthreads();
+    prefix |= (uint32_t)part[16] << shift;
+    want = part[17];
+    __syncthreads();
+  }
+  // ---- a bit per slot: above the n-th key, equal to it (want of those stay, the lowest)
+  each([&](int t, uint32_t k) __attribute__((always_inline)) {
+    const uint64_t a = __ballot(t < L && k > prefix), e = __ballot(t < L && k == prefix);
+    if (lane == 0 && (t >> 6) < p.words) above[t >> 6] = a, equal[t >> 6] = e;
+  });
+  __syncthreads();
+  const int words = (L + 63) >> 6;
+  for (int w0 = 0, ties = 0, gaps = 0; w0 < words; w0 += kChooseThreads) {
+    const int w = w0 + tid;
+    const uint64_t e = w < words ? equal[w] : 0;
+    int total;
+    const int upto = scan_threads(ones(e), part, &total);
+    int take = want - (ties + upto - ones(e));  // of this word's ties
+    uint64_t kept = 0;
+    if (w < words) {
+      kept = above[w];
+      if (take >= ones(e)) kept |= e;
+      else if (take > 0) kept |= e & ((1ull << select_bit(e, take)) - 1);
+      above[w] = kept;
+    }
+    ties += total;
+    const int low = n - w * 64;  // slots of this word below n
+    const uint64_t gap = w < words && low > 0 ? ~kept & (low >= 64 ? ~0ull : (1ull << low) - 1) : 0;
+    const int g = scan_threads(ones(gap), part, &total);
+    if (w < words) before[w] = gaps + g - ones(gap);
+    gaps += total;
+  }
+  __syncthreads();
+  // ---- the map: a wave per word of slots
+  const int first = n >> 6;  // the word n lies in
+  // kept slots from n on, counted: those before word w are n's worth of gaps filled; their number is the gaps' by then
+  for (int w = wave; w < words; w += kChooseWaves) {
+    const uint64_t kept = above[w];
+    const int t = w * 64 + lane;
+    if (t < n && (kept >> lane & 1)) src[t] = t;
+  }
+  for (int w0 = first, late = 0; w0 < words; w0 += kChooseThreads) {  // late: kept slots from n on before these words
+    const int w = w0 + tid;
+    uint64_t kept = w < words ? above[w] : 0;
+    if (w == first) kept &= ~0ull << (n & 63);
+    int total;
+    int rank = late + scan_threads(ones(kept), part, &total) - ones(kept);
+    late += total;
+    while (kept) {
+      const int t = w * 64 + __builtin_ctzll(kept);
+      kept &= kept - 1;
+      // the word that holds gap number `rank`: the last one with before <= rank
+      int lo = 0, hi = (n - 1) >> 6;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= rank) lo = mid;
+        else hi = mid - 1;
+      }
+      const int low = n - lo * 64;
+      const uint64_t gap = ~above[lo] & (low >= 64 ? ~0ull : (1ull << low) - 1);
+      src[lo * 64 + select_bit(gap, rank - before[lo])] = t;
+      ++rank;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// the move
+// ---------------------------------------------------------------------------------------
+struct ShiftParams {
+  const int32_t *n, *src;
+  CacheView c;
+  float *weight;
+  int32_t *pos, *err_flag;
+  int64_t ld, ld_src, layer_cache;  // layer_cache: units
+  int B, H, Hkv, max_keep;
+};
+
+constexpr int kShiftWaves = 4;
+
+// Grid: 256 slots, (sequence, head), layer; a wave takes 64 slots.
+template <int D, int KIND>
+__global__ void __launch_bounds__(64 * kShiftWaves) shift_kernel(const ShiftParams p) {
+  constexpr int ROW = KIND == TVA_ROWS_BF16 ? D * 2 : KIND == TVA_ROWS_E4M3 ? D : D / 2;  // bytes
+  constexpr int UNIT = KIND == TVA_ROWS_BF16 ? 2 : KIND == TVA_ROWS_E4M3 ? 1 : D / 2;
+  constexpr int LPR = ROW / 16, RPI = 64 / LPR;  // lanes per row, rows at once
+  __shared__ int64_t froms[kShiftWaves][64], tos[kShiftWaves][64];
+  const int b = blockIdx.y / p.Hkv, g = blockIdx.y - b * p.Hkv, layer = blockIdx.z;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int n = min(p.n[b], p.max_keep);
+  const int j = (blockIdx.x * kShiftWaves + wave) * 64 + lane;
+  const int64_t r = ((int64_t)layer * p.B + b) * p.H + (p.H == 1 ? 0 : g);
+  if (j - lane >= n) return;  // (a wave at a time; no barriers)
+  const int old = j < n ? p.src[r * p.ld_src + j] : j;
+  const int64_t room = room_of(p.c, b);
+  const bool wrong = j < n && old != j && (old < p.n[b] || old >= room || j >= room || ((p.weight || p.pos) && old >= p.ld));
+  if (wrong && p.err_flag) atomicCAS(p.err_flag, 0, 1 + b);
+  const bool moves = j < n && old != j && !wrong;
+  const uint64_t who = __ballot(moves);
+  const int count = ones(who);
+  if (moves) {
+    const int at = ones(who & ((1ull << lane) - 1));
+    const int64_t base = layer * p.layer_cache + g * p.c.stride_head;
+    froms[wave][at] = base + position_at(p.c, b, old), tos[wave][at] = base + position_at(p.c, b, j);
+    if (p.H != 1 || g == 0) {
+      if (p.weight) p.weight[r * p.ld + j] = p.weight[r * p.ld + old];
+      if (p.pos) p.pos[r * p.ld + j] = p.pos[r * p.ld + old];
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int piece = (lane % LPR) * 16;
+#pragma unroll 2
+  for (int i = lane / LPR; i < count; i += RPI) {
+    const int64_t from = froms[wave][i], to = tos[wave][i];
+    const u32x4 k = *(const u32x4 *)(p.c.k + from * UNIT + piece), v = *(const u32x4 *)(p.c.v + from * UNIT + piece);
+    *(u32x4 *)(p.c.k + to * UNIT + piece) = k;
+    *(u32x4 *)(p.c.v + to * UNIT + piece) = v;
+    if constexpr (KIND == TVA_ROWS_E2M1) {
+      if (lane % LPR == 0) {
+        if constexpr (D == 128) ((uint32_t *)p.c.k_row_scale)[to] = ((const uint32_t *)p.c.k_row_scale)[from];
+        else ((uint16_t *)p.c.k_row_scale)[to] = ((const uint16_t *)p.c.k_row_scale)[from];
+        ((uint16_t *)p.c.v_row_scale)[to] = ((const uint16_t *)p.c.v_row_scale)[from];
+      }
+    }
+  }
+}
+
+template <class F>
+int by_kind(int D, int kind, F f) {
+  auto of = [&](auto d) {
+    if (kind == TVA_ROWS_BF16) f(d, std::integral_constant<int, TVA_ROWS_BF16>{});
+    else if (kind == TVA_ROWS_E4M3) f(d, std::integral_constant<int, TVA_ROWS_E4M3>{});
+    else f(d, std::integral_constant<int, TVA_ROWS_E2M1>{});
+  };
+  if (D == 128) of(std::integral_constant<int, 128>{});
+  else of(std::integral_constant<int, 64>{});
+  return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tva_key_weights(const tva_key_weight_args *a, void *stream) {
+  if (!a || a->B < 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv || a->max_rows < 0 || a->max_L < 0) return TVA_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (!(a->scale > 0.f) || a->ld < a->max_L) return TVA_INVALID_ARG;
+  if (a->B == 0 || a->max_rows == 0 || a->max_L == 0) return TVA_OK;
+  if (!a->cu_T || !a->L || !a->q || !a->lse || !a->weight || (a->path == nullptr) != (a->path_len == nullptr)) return TVA_INVALID_ARG;
+  if (((uintptr_t)a->q & 15) || (a->pos && !a->first_pos)) return TVA_INVALID_ARG;
+  WeighParams p{};
+  const int rc = view_of(a->cache, a->Hkv, a->D, false, &p.c);
+  if (rc != TVA_OK) return rc;
+  p.cu_T = a->cu_T, p.path = a->path, p.path_len = a->path_len, p.L = a->L, p.first_pos = a->first_pos;
+  p.q = (const __bf16 *)a->q, p.lse = a->lse, p.weight = a->weight, p.pos = a->pos, p.ld = a->ld;
+  p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.max_rows = a->max_rows, p.max_L = a->max_L;
+  const float ks = a->cache.kind == TVA_ROWS_E4M3 && a->cache.k_scale != 0.f ? a->cache.k_scale : 1.f;
+  p.scale_log2 = a->scale * ks * kLog2e;
+  const int64_t blocks = ((int64_t)a->max_L + 128 - 1) / 128;
+  if (a->B > 65535 || blocks > 65535) return TVA_UNSUPPORTED;
+  (void)hipGetLastError();
+  return by_kind(a->D, a->cache.kind, [&](auto d, auto kind) {
+    hipLaunchKernelGGL((weigh_kernel<decltype(d)::value, decltype(kind)::value, 1>), dim3(a->Hkv, (unsigned)blocks, a->B), dim3(64 * kWeighWaves), 0,
+                       (hipStream_t)stream, p);
+  });
+}
+size_t tva_sizeof_key_weight_args(void) { return sizeof(tva_key_weight_args); }
+
+int tva_evict_select(const tva_evict_select_args *a, void *stream) {
+  if (!a || a->B < 0 || a->H < 1 || a->max_L < 0 || a->n_layers < 0 || a->n_first < 0) return TVA_INVALID_ARG;
+  if (a->max_L > TVA_EVICT_MAX_SLOTS) return TVA_UNSUPPORTED;
+  if (a->ld < a->max_L || a->ld_src < 0) return TVA_INVALID_ARG;
+  if (a->B == 0) return TVA_OK;
+  if (!a->L || !a->keep || !a->weight || !a->src) return TVA_INVALID_ARG;
+  if (a->L_out && (a->L_out == a->L || a->L_out == a->keep)) return TVA_INVALID_ARG;
+  const int layers = a->n_layers > 0 ? a->n_layers : 1;
+  if (a->B > 65535 || layers > 65535) return TVA_UNSUPPORTED;
+  ChooseParams p{};
+  p.L = a->L, p.keep = a->keep, p.newest = a->newest, p.pos = a->pos, p.weight = a->weight, p.src = a->src, p.L_out = a->L_out;
+  p.ld = a->ld, p.ld_src = a->ld_src, p.B = a->B, p.H = a->H, p.max_L = a->max_L, p.n_first = a->n_first;
+  p.words = (a->max_L + 63) / 64;
+  const size_t bytes = (size_t)p.words * 20 + (256 * kCopies + 32) * 4;
+  const dim3 grid(a->H, a->B, layers), block(kChooseThreads);
+  const hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  if (a->max_L <= 4 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<4>, grid, block, bytes, st, p);
+  else if (a->max_L <= 32 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<32>, grid, block, bytes, st, p);
+  else hipLaunchKernelGGL(choose_kernel<0>, grid, block, bytes, st, p);
+  return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
+}
+size_t tva_sizeof_evict_select_args(void) { return sizeof(tva_evict_select_args); }
+
+int tva_evict_move(const tva_evict_move_args *a, void *stream) {
+  if (!a || a->B < 0 || a->Hkv < 1 || a->max_keep < 0 || a->n_layers < 0 || (a->H != 1 && a->H != a->Hkv)) return TVA_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (a->ld_src < a->max_keep || a->layer_stride_cache < 0 || ((a->weight || a->pos) && a->ld < a->max_keep)) return TVA_INVALID_ARG;
+  if (a->B == 0 || a->max_keep == 0) return TVA_OK;
+  if (!a->n || !a->src) return TVA_INVALID_ARG;
+  ShiftParams p{};
+  const int rc = view_of(a->cache, a->Hkv, a->D, true, &p.c);
+  if (rc != TVA_OK) return rc;
+  const int unit = a->cache.kind == TVA_ROWS_E2M1 ? a->D : a->cache.kind == TVA_ROWS_E4M3 ? 16 : 8;
+  if (a->layer_stride_cache % unit) return TVA_INVALID_ARG;
+  const int layers = a->n_layers > 0 ? a->n_layers : 1;
+  if ((int64_t)a->B * a->Hkv > 65535 || layers > 65535) return TVA_UNSUPPORTED;
+  p.n = a->n, p.src = a->src, p.weight = a->weight, p.pos = a->pos, p.err_flag = a->err_flag, p.ld = a->ld, p.ld_src = a->ld_src;
+  p.layer_cache = a->cache.kind == TVA_ROWS_E2M1 ? a->layer_stride_cache / a->D : a->layer_stride_cache;
+  p.B = a->B, p.H = a->H, p.Hkv = a->Hkv, p.max_keep = a->max_keep;
+  const dim3 grid((a->max_keep + 64 * kShiftWaves - 1) / (64 * kShiftWaves), a->B * a->Hkv, layers);
+  (void)hipGetLastError();
+  return by_kind(a->D, a->cache.kind, [&](auto d, auto kind) {
+    hipLaunchKernelGGL((shift_kernel<decltype(d)::value, decltype(kind)::value>), grid, dim3(64 * kShiftWaves), 0, (hipStream_t)stream, p);
+  });
+}
+size_t tva_sizeof_evict_move_args(void) { return sizeof(tva_evict_move_args); }
+
+}  // extern "C"
