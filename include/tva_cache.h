@@ -100,6 +100,9 @@ typedef struct tva_attn4_args {
   int32_t max_L;          /* host-side bound of L[b] (a value below some L[b] truncates that sequence's context) */
   float scale;
   int32_t num_splits;
+  int32_t plan_rows;           /* query rows (nodes x heads of a KV head) per workgroup: 32, 64 or 128; 0 = the library chooses.  A
+                                  tuning and testing aid: every value computes the same for every input, in another order */
+  int32_t reserved;
   const int32_t *cu_T, *L;     /* device [B+1], [B] */
   const void *q;               /* device bf16 [sum_T, Hq, D] */
   const void *k_tree, *v_tree; /* device bf16 [sum_T, Hkv, D] */

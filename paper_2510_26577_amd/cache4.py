@@ -33,7 +33,7 @@ class RowsArgs(ctypes.Structure):
 class Attn4Args(ctypes.Structure):
     """Mirror of `struct tva_attn4_args`."""
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "D", "sum_T", "max_T", "mask_words", "max_L")] + \
-               [("scale", ctypes.c_float), ("num_splits", ctypes.c_int32)] + \
+               [("scale", ctypes.c_float), ("num_splits", ctypes.c_int32), ("plan_rows", ctypes.c_int32), ("reserved", ctypes.c_int32)] + \
                [(n, ctypes.c_void_p) for n in ("cu_T", "L", "q", "k_tree", "v_tree", "anc_mask", "parent")] + \
                [("cache", Cache), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t)]
@@ -108,13 +108,13 @@ def load(*, stream=None, **kw) -> None:
 
 
 def make_attn_args(*, q, k_tree, v_tree, cache: Cache, cu_T, L, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
-                   lse=None, workspace=None, num_splits: int = 0) -> Attn4Args:
+                   lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0) -> Attn4Args:
     """q bf16 [sum_T, Hq, D], k_tree / v_tree bf16 [sum_T, Hkv, D], out bf16 like q, lse fp32 [sum_T, Hq] or None."""
     a = Attn4Args()
     a.B = cu_T.numel() - 1
     a.sum_T, a.Hq, a.D = (int(s) for s in q.shape)
     a.Hkv = int(k_tree.shape[1])
-    a.max_T, a.max_L, a.num_splits = int(max_T), int(max_L), int(num_splits)
+    a.max_T, a.max_L, a.num_splits, a.plan_rows = int(max_T), int(max_L), int(num_splits), int(plan_rows)
     a.mask_words = int(anc_mask.shape[1]) if anc_mask is not None else max(1, (int(max_T) + 63) // 64)
     a.scale = float(scale)
     a.cu_T, a.L, a.q, a.k_tree, a.v_tree = _p(cu_T), _p(L), _p(q), _p(k_tree), _p(v_tree)
@@ -155,7 +155,7 @@ def tree_verify_attn_raw(args: Attn4Args, stream=None) -> None:
 
 
 def tree_verify_attn(q, k_tree, v_tree, cache: Cache, cu_T, L, *, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
-                     lse=None, workspace=None, num_splits: int = 0, stream: Optional[object] = None):
+                     lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0, stream: Optional[object] = None):
     """Tree-masked verification attention over a cache of 4-bit rows.  Returns (out bf16 [sum_T, Hq, D], lse fp32 [sum_T, Hq])."""
     import torch
     if out is None:
@@ -163,7 +163,7 @@ def tree_verify_attn(q, k_tree, v_tree, cache: Cache, cu_T, L, *, max_T: int, ma
     if lse is None:
         lse = torch.empty(tuple(q.shape[:2]), dtype=torch.float32, device=q.device)
     a = make_attn_args(q=q, k_tree=k_tree, v_tree=v_tree, cache=cache, cu_T=cu_T, L=L, max_T=max_T, max_L=max_L, scale=scale, anc_mask=anc_mask,
-                       parent=parent, out=out, lse=lse, workspace=workspace, num_splits=num_splits)
+                       parent=parent, out=out, lse=lse, workspace=workspace, num_splits=num_splits, plan_rows=plan_rows)
     ws = attn_workspace(a, q.device) if workspace is None else None
     tree_verify_attn_raw(a, stream)
     if ws is not None and stream is not None:  # it goes back to the current stream's pool: not before the work on `stream` is done

@@ -25,6 +25,7 @@ namespace {
 using namespace cache_rows;
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -146,6 +147,7 @@ struct FourParams {
   float *lse;
   float *part_out, *part_lse;  // [S, sum_T * Hq, D], [S, sum_T * Hq] when S > 1
   int Hq, Hkv, G, W, sum_T, max_L, S, chunk;  // chunk: keys per split, a multiple of 64
+  int tree_split;                             // the split of its own that the tree's keys have, or -1: the last one with cached keys has them
   float scale_log2;
 };
 
@@ -194,7 +196,11 @@ struct FourCfg {
   static constexpr int RPL = 64 / CH;        // rows such a load covers
   static constexpr int KL = RB / 32;         // 16-byte pieces of a lane's half of a K row
   static constexpr int VT = 64 * RB;         // V tile
-  static constexpr int WAVE_LDS = VT + 256;  // V tile and its 64 scales
+  // a wave's LDS: the V tile and its 64 scales; for a tree tile, NB blocks of bf16 rows n, n + NB, n + 2 NB ..., 32 bytes apart, so
+  // that the four consecutive rows a transposing read takes together are in different banks
+  static constexpr int NB = D / 8, BLK = 1024 + 32;
+  static constexpr int WAVE_LDS = NB * BLK;
+  static_assert(VT + 256 <= WAVE_LDS, "");
   static constexpr int TP = D + 4;           // floats between rows of an output patch
   static constexpr int PATCH = 32 * TP * 4;
   static constexpr int EXCHANGE = 2 * kWaves * 32 * 4;  // maxima and sums
@@ -221,8 +227,8 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   const int L = min(max(p.L[b], 0), p.max_L);
   const int last_split = L > 0 ? (L - 1) / p.chunk : 0;
   const int key0 = split * p.chunk;
-  const int n_keys = split <= last_split ? min(p.chunk, L - key0) : 0;
-  const bool has_tree = split == last_split;
+  const int n_keys = split <= last_split && split != p.tree_split ? min(p.chunk, L - key0) : 0;
+  const bool has_tree = split == (p.tree_split < 0 ? last_split : p.tree_split);
   const int n_cache = (n_keys + 63) >> 6, n_tiles = n_cache + (has_tree ? (T + 63) >> 6 : 0);
 
   // this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written
@@ -237,7 +243,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
   float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
 
-  if (n_tiles > 0 && split <= last_split) {
+  if (n_tiles > 0) {
     // ancestor set of this lane's node, trimmed to the tree
     uint64_t anc0 = 0, anc1 = 0;
     if (has_tree) {
@@ -261,11 +267,6 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
       if (T < 64) anc0 &= (1ull << T) - 1, anc1 = 0;
       else if (T < 128) anc1 &= (1ull << (T - 64)) - 1;
     }
-
-    bf16x8 q[C::NS];
-    const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
-#pragma unroll
-    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(qrow + s * 8);
 
     unsigned char *vt = lds + wave * C::WAVE_LDS;
     float *vsl = (float *)(vt + C::VT);
@@ -311,6 +312,14 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
       vs = *(const uint16_t *)(p.c.v_row_scale + rs * 2);
     };
 
+    int tile = wk;
+    if (!idle && tile < n_cache) fetch(tile);
+    bf16x8 q[C::NS];
+    const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(qrow + s * 8);
+
+
     f32x16 s[2];
     // scores -> probabilities in place (log2 domain, fp32), O and l moved to a new reference where a row's maximum grew
     auto soften = [&]() __attribute__((always_inline)) {
@@ -341,8 +350,6 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     };
 
     if (!idle) {
-      int tile = wk;
-      if (tile < n_cache) fetch(tile);
       for (; tile < n_cache; tile += WK) {
         // ---- V to LDS: piece c of row r lies at piece c ^ (r / 8) of its row, so that the 16 rows a transposing read takes
         // together (4 consecutive ones of each 8) are in different banks
@@ -397,9 +404,17 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
           }
         }
       }
-      // ---- the tree's own keys, bf16
+      // ---- the tree's own keys, bf16: V goes to LDS while K's rows are fetched and multiplied
       for (; tile < n_tiles; tile += WK) {
         const int first = (tile - n_cache) * 64, left = T - first;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int n = 0; n < C::NB; ++n) {
+          const int r = first + n + C::NB * (lane / C::NB);
+          const __bf16 *from = p.v_tree + ((int64_t)(t0 + min(r, T - 1)) * p.Hkv + g) * D + (lane % C::NB) * 8;
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                           (__attribute__((address_space(3))) void *)(vt + n * C::BLK), 16, 0, 0);
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -418,6 +433,8 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
             if (!((bits >> (8 * (i / 4) + 4 * half + i % 4)) & 1)) s[kb][i] = -INFINITY;
         }
         soften();
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): V is in LDS
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -426,14 +443,18 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
             bf16x8 w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[kb][a * 8 + i];
+            // 16 lanes turn over 4 rows x 16 elements: this lane's row (of keys 8 c + 4 half + 0..3) and 8-byte piece of it
+            const int i16 = lane & 15, sub = (lane >> 4) & 1;
 #pragma unroll
             for (int j = 0; j < C::NJ; ++j) {
-              bf16x8 v;
+              s16x4 c[2];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int key = first + kb * 32 + a * 16 + 8 * (i / 4) + 4 * half + i % 4;
-                v[i] = p.v_tree[((int64_t)(t0 + min(key, T - 1)) * p.Hkv + g) * D + j * 32 + l32];
+              for (int h = 0; h < 2; ++h) {
+                const int r = 32 * kb + 16 * a + 8 * h + 4 * half + (i16 >> 2);
+                c[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4 *)(vt + (r % C::NB) * C::BLK + (r / C::NB) * (D * 2) + j * 64 + sub * 32 + (i16 & 3) * 8));
               }
+              bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
               add_infinite(v, w, acc[j]);
               acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
             }
@@ -497,25 +518,39 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   }
 }
 
-// Splits of one row per D/4 lanes: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s.
+// Splits of one row per D/4 lanes: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s.  Eight splits are in flight at a
+// time; what a split without keys holds is read and dropped.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const float *part_out, const float *part_lse, int S, int64_t n, __bf16 *out, float *lse) {
-  constexpr int LPR = D / 4;
+  constexpr int LPR = D / 4, U = 8;
   const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int d = (threadIdx.x % LPR) * 4;
   if (row >= n) return;
-  float top = -INFINITY;
-  for (int s = 0; s < S; ++s) top = fmaxf(top, part_lse[s * n + row]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-  for (int s = 0; s < S; ++s) {
-    const float ls = part_lse[s * n + row];
-    if (ls == -INFINITY) continue;  // (nothing was written there)
-    const float w = __builtin_amdgcn_exp2f((ls - top) * kLog2e);
-    sum += w;
-    o += *(const f32x4 *)(part_out + (s * n + row) * D + d) * w;
+  float top = -INFINITY, sum = 0.f;
+  for (int s0 = 0; s0 < S; s0 += U) {
+    float ls[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = (int64_t)min(s0 + u, S - 1) * n + row;
+      ls[u] = part_lse[at];
+      x[u] = *(const f32x4 *)(part_out + at * D + d);
+    }
+    float here = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) here = fmaxf(here, ls[u]);
+    const float f = here == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - here) * kLog2e);
+    o *= f, sum *= f, top = here;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + u >= S || ls[u] == -INFINITY) continue;  // (nothing was written there)
+      const float w = __builtin_amdgcn_exp2f((ls[u] - (top == -INFINITY ? 0.f : top)) * kLog2e);
+      sum += w;
+      o += x[u] * w;
+    }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   bf16x4 y;
 #pragma unroll
@@ -526,31 +561,36 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part_out, const 
 
 struct FourPlan {
   int WM, blocks, S, chunk;
+  bool tree_alone;
 };
-bool plan_four(const tva_attn4_args *a, FourPlan *pl) {
+void plan_four(const tva_attn4_args *a, FourPlan *pl) {
   const int G = a->Hq / a->Hkv;
-  const int64_t rows = (int64_t)a->max_T * G;
-  const int groups = (int)((rows + 31) / 32);
-  pl->WM = groups >= 3 ? 4 : groups == 2 ? 2 : 1;
-  pl->blocks = (int)((rows + pl->WM * 32 - 1) / (pl->WM * 32));
+  const int64_t rows = (int64_t)a->max_T * G, groups = std::max<int64_t>(1, (rows + 31) / 32);
   const int tiles = std::max(1, (a->max_L + 63) / 64);
-  const int64_t base = std::max<int64_t>(1, (int64_t)a->B * a->Hkv * pl->blocks);
+  const int64_t pairs = (int64_t)a->B * a->Hkv;
+  if (a->plan_rows) pl->WM = a->plan_rows / 32;
+  else pl->WM = pairs * groups * tiles <= 4 * 2048 || groups == 1 ? 1 : groups % 4 == 0 || groups > 8 ? 4 : groups % 2 == 0 ? 2 : groups == 3 ? 4 : 1;
+  pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
+  const int64_t base = pairs * pl->blocks;
+  const int WK = kWaves / pl->WM;
   int64_t S = a->num_splits;
   if (S == 0) {
-    S = (512 + base - 1) / base;                            // two workgroups per CU
-    S = std::min<int64_t>(S, std::max(1, tiles * pl->WM / kWaves));  // a tile per wave
+    S = (512 + base - 1) / base;                                      // two workgroups per CU
+    S = std::min<int64_t>(S, std::max(1, (tiles + WK - 1) / WK));  // a tile per wave
   }
   S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
   const int per = (int)((tiles + S - 1) / S);
   pl->chunk = per * 64;
   pl->S = (tiles + per - 1) / per;
-  return true;
+  pl->tree_alone = pl->S > 1;
+  pl->S += pl->tree_alone;
 }
 
 int check_four(const tva_attn4_args *a, bool shapes_only) {
   if (!a || a->B <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv) return TVA_INVALID_ARG;
   if (a->sum_T < 0 || a->max_T < 0 || a->max_L < 0 || a->num_splits < 0) return TVA_INVALID_ARG;
   if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (a->plan_rows != 0 && a->plan_rows != 32 && a->plan_rows != 64 && a->plan_rows != 128) return TVA_INVALID_ARG;
   if (a->max_T > TVA_MAX_TREE) return TVA_UNSUPPORTED;
   if (a->max_L > 0x7fffff00) return TVA_UNSUPPORTED;  // (positions are rounded up to whole tiles)
   if (shapes_only) return TVA_OK;
@@ -610,13 +650,15 @@ size_t tva_sizeof_rows_args(void) { return sizeof(tva_rows_args); }
 
 size_t tva_attn4_workspace_bytes(const tva_attn4_args *a) {
   FourPlan pl;
-  if (check_four(a, true) != TVA_OK || !plan_four(a, &pl)) return (size_t)-1;
+  if (check_four(a, true) != TVA_OK) return (size_t)-1;
+  plan_four(a, &pl);
   return four_bytes(a, pl);
 }
 
 int32_t tva_attn4_plan_splits(const tva_attn4_args *a) {
   FourPlan pl;
-  if (check_four(a, true) != TVA_OK || !plan_four(a, &pl)) return -1;
+  if (check_four(a, true) != TVA_OK) return -1;
+  plan_four(a, &pl);
   return pl.S;
 }
 
@@ -639,7 +681,7 @@ int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream) {
   const int64_t n = (int64_t)a->sum_T * a->Hq;
   p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (pl.S > 1 ? pl.S * n * a->D : 0);
   p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.sum_T = a->sum_T, p.max_L = a->max_L;
-  p.S = pl.S, p.chunk = pl.chunk, p.scale_log2 = a->scale * kLog2e;
+  p.S = pl.S, p.chunk = pl.chunk, p.tree_split = pl.tree_alone ? pl.S - 1 : -1, p.scale_log2 = a->scale * kLog2e;
   const dim3 grid(a->Hkv, pl.blocks, a->B * pl.S);
   const hipStream_t st = (hipStream_t)stream;
   const bool paged = a->cache.page_table != nullptr;
