@@ -183,17 +183,18 @@ __device__ __forceinline__ int select_bit(uint64_t w, int r) {
 }
 
 // Inclusive sum over the workgroup's threads, and its total
-__device__ __forceinline__ int scan_threads(int x, int *part, int *total) {
+template <class T>
+__device__ __forceinline__ T scan_threads(T x, T *part, T *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
-    const int y = __shfl_up(x, o);
+    const T y = __shfl_up(x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();  // (part may still be read)
   if (lane == 63) part[wave] = x;
   __syncthreads();
-  int before = 0, all = 0;
+  T before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kChooseWaves; ++w) {
     before += w < wave ? part[w] : 0;
@@ -208,9 +209,11 @@ template <int ITEMS>
 __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseParams p) {
   extern __shared__ __align__(16) unsigned char lds[];
   uint64_t *above = (uint64_t *)lds, *equal = above + p.words;  // a bit per slot; above becomes the kept set
-  int *before = (int *)(equal + p.words);                        // gaps before each word
-  int *hist = before + p.words;                                  // [256][kCopies]
-  int *part = hist + 256 * kCopies;                              // 16, and 4 words of the search
+  uint64_t *part64 = equal + p.words;                            // kChooseWaves
+  int *before = (int *)(part64 + kChooseWaves);                  // gaps before each word
+  int *rank0 = before + p.words;                                 // kept slots from n on before each word
+  int *hist = rank0 + p.words;                                   // [256][kCopies]
+  int *part = hist + 256 * kCopies;                              // kChooseWaves, and what a pass finds
   const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int L = min(max(p.L[b], 0), p.max_L), n = (int)min((int64_t)min(max(p.keep[b], 0), L), p.ld_src);
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
     int mine = 0;
     const int digit = 255 - tid;  // thread 0 has the largest
     if (tid < 256)
-      for (int c = 0; c < kCopies; ++c) mine += hist[digit * kCopies + c];
+      for (int c = 0; c < kCopies; ++c) mine += hist[digit * kCopies + ((c + lane) & (kCopies - 1))];
     int total;
     const int upto = scan_threads(mine, part, &total);
     if (tid < 256 && upto >= want && upto - mine < want) part[16] = digit, part[17] = want - (upto - mine);
@@ -281,57 +284,47 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   });
   __syncthreads();
   const int words = (L + 63) >> 6;
-  for (int w0 = 0, ties = 0, gaps = 0; w0 < words; w0 += kChooseThreads) {
+  for (int w0 = 0, ties = 0, gaps = 0, late = 0; w0 < words; w0 += kChooseThreads) {
     const int w = w0 + tid;
     const uint64_t e = w < words ? equal[w] : 0;
     int total;
     const int upto = scan_threads(ones(e), part, &total);
-    int take = want - (ties + upto - ones(e));  // of this word's ties
-    uint64_t kept = 0;
-    if (w < words) {
-      kept = above[w];
-      if (take >= ones(e)) kept |= e;
-      else if (take > 0) kept |= e & ((1ull << select_bit(e, take)) - 1);
-      above[w] = kept;
-    }
+    const int take = want - (ties + upto - ones(e));  // of this word's ties
     ties += total;
+    uint64_t kept = w < words ? above[w] : 0;
+    if (take >= ones(e)) kept |= e;
+    else if (take > 0) kept |= e & ((1ull << select_bit(e, take)) - 1);
     const int low = n - w * 64;  // slots of this word below n
-    const uint64_t gap = w < words && low > 0 ? ~kept & (low >= 64 ? ~0ull : (1ull << low) - 1) : 0;
-    const int g = scan_threads(ones(gap), part, &total);
-    if (w < words) before[w] = gaps + g - ones(gap);
-    gaps += total;
+    const uint64_t below = low >= 64 ? ~0ull : low > 0 ? (1ull << low) - 1 : 0;
+    // gaps below n in the low half, kept slots from n on in the high half: neither sum passes 2^18
+    const uint64_t mine = w < words ? (uint64_t)ones(~kept & below) | (uint64_t)ones(kept & ~below) << 32 : 0;
+    uint64_t all;
+    const uint64_t sums = scan_threads(mine, part64, &all) - mine;
+    if (w < words) above[w] = kept, before[w] = gaps + (int)sums, rank0[w] = late + (int)(sums >> 32);
+    gaps += (int)all, late += (int)(all >> 32);
   }
   __syncthreads();
-  // ---- the map: a wave per word of slots
-  const int first = n >> 6;  // the word n lies in
-  // kept slots from n on, counted: those before word w are n's worth of gaps filled; their number is the gaps' by then
+  // ---- the map: a wave per word of slots; the m-th kept slot from n on goes to the m-th gap
   for (int w = wave; w < words; w += kChooseWaves) {
     const uint64_t kept = above[w];
     const int t = w * 64 + lane;
-    if (t < n && (kept >> lane & 1)) src[t] = t;
-  }
-  for (int w0 = first, late = 0; w0 < words; w0 += kChooseThreads) {  // late: kept slots from n on before these words
-    const int w = w0 + tid;
-    uint64_t kept = w < words ? above[w] : 0;
-    if (w == first) kept &= ~0ull << (n & 63);
-    int total;
-    int rank = late + scan_threads(ones(kept), part, &total) - ones(kept);
-    late += total;
-    while (kept) {
-      const int t = w * 64 + __builtin_ctzll(kept);
-      kept &= kept - 1;
-      // the word that holds gap number `rank`: the last one with before <= rank
-      int lo = 0, hi = (n - 1) >> 6;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (before[mid] <= rank) lo = mid;
-        else hi = mid - 1;
-      }
-      const int low = n - lo * 64;
-      const uint64_t gap = ~above[lo] & (low >= 64 ? ~0ull : (1ull << low) - 1);
-      src[lo * 64 + select_bit(gap, rank - before[lo])] = t;
-      ++rank;
+    if (!(kept >> lane & 1)) continue;
+    if (t < n) {
+      src[t] = t;
+      continue;
     }
+    const int low = n - w * 64;
+    const uint64_t here = low > 0 ? kept & (~0ull << low) : kept;
+    const int rank = rank0[w] + ones(here & ((1ull << lane) - 1));
+    int lo = 0, hi = (n - 1) >> 6;  // the word that holds the gap: the last one with before <= rank
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before[mid] <= rank) lo = mid;
+      else hi = mid - 1;
+    }
+    const int room = n - lo * 64;
+    const uint64_t gap = ~above[lo] & (room >= 64 ? ~0ull : (1ull << room) - 1);
+    src[lo * 64 + select_bit(gap, rank - before[lo])] = t;
   }
 }
 
@@ -450,7 +443,7 @@ int tva_evict_select(const tva_evict_select_args *a, void *stream) {
   p.L = a->L, p.keep = a->keep, p.newest = a->newest, p.pos = a->pos, p.weight = a->weight, p.src = a->src, p.L_out = a->L_out;
   p.ld = a->ld, p.ld_src = a->ld_src, p.B = a->B, p.H = a->H, p.max_L = a->max_L, p.n_first = a->n_first;
   p.words = (a->max_L + 63) / 64;
-  const size_t bytes = (size_t)p.words * 20 + (256 * kCopies + 32) * 4;
+  const size_t bytes = (size_t)p.words * 24 + kChooseWaves * 8 + (256 * kCopies + 32) * 4;
   const dim3 grid(a->H, a->B, layers), block(kChooseThreads);
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
