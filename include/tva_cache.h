@@ -35,6 +35,7 @@ typedef enum {
  * The first element of KV head g of a position is element page*stride_page + slot*stride_tok + g*stride_head, strides
  * counted in ELEMENTS whatever the kind (page = 0, slot = row in the dense form).  0 = the packed default, [.., Hkv, D]
  * token-major.  BF16: multiples of 8, E4M3: of 16, E2M1: of D (a row's scales are found by element / D).
+ * Positions are below 2^30; E2M1 row numbers (element / D) below 2^32.
  * Head-major ([.., Hkv, page_size, D]: stride_tok = D, stride_head = page_size*D) keeps a head's keys together.
  */
 typedef struct tva_cache {

@@ -275,30 +275,29 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     u32x4 kx[2][C::KL], vx[C::CH];
     uint32_t ks[2];
     uint16_t vs;
-    const int64_t head_rows = g * p.c.stride_head;
-    const int64_t dense0 = PAGED ? 0 : (int64_t)p.c.cu_L[b] * p.c.stride_tok + head_rows;
-    // row numbers of the tile's keys: K's (this lane's key in each block of 32), V's (the rows its loads cover), and key `lane`
-    auto row_of = [&](int key) __attribute__((always_inline)) -> int64_t {
-      const int t = key0 + min(key, n_keys - 1);  // rows past the end repeat the last one and are masked
-      if constexpr (PAGED) return position_at(p.c, b, t) + head_rows;
-      else return dense0 + (int64_t)t * p.c.stride_tok;
+    const Finder<PAGED> find(p.c, b, g);
+    // a tile's rows past the end repeat the last one and are masked
+    auto own = [&](int key) __attribute__((always_inline)) { return key0 + min(key, n_keys - 1); };
+    // rows of the tile's keys: K's (this lane's key in each block of 32), V's (the rows its loads cover), and key `lane`; paged: each
+    // lane has the table entry of key `lane`, looked up a tile earlier, and hands its row to the others
+    int entry = 0;
+    auto look = [&](int tile) __attribute__((always_inline)) {
+      if constexpr (PAGED) entry = find.entry(p.c, own(tile * 64 + lane));
     };
     auto fetch = [&](int tile) __attribute__((always_inline)) {
-      int64_t rk[2], rv[C::CH], rs;
-      if constexpr (PAGED) {  // one table entry per key, handed out among the lanes
-        rs = row_of(tile * 64 + lane);
-        const int lo = (int)rs, hi = (int)(rs >> 32);
-        auto of = [&](int l) __attribute__((always_inline)) { return ((int64_t)__shfl(hi, l) << 32) | (uint32_t)__shfl(lo, l); };
+      int64_t rk[2], rv[C::CH];
+      const int64_t rs = find.at(p.c, own(tile * 64 + lane), entry);
+      if constexpr (PAGED) {
+        auto of = [&](int l) __attribute__((always_inline)) { return (int64_t)(uint32_t)__shfl((int)rs, l); };  // (row numbers have 32 bits)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) rk[kb] = of(kb * 32 + l32);
 #pragma unroll
         for (int i = 0; i < C::CH; ++i) rv[i] = of(i * C::RPL + lane / C::CH);
       } else {
-        rs = row_of(tile * 64 + lane);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) rk[kb] = row_of(tile * 64 + kb * 32 + l32);
+        for (int kb = 0; kb < 2; ++kb) rk[kb] = find.at(p.c, own(tile * 64 + kb * 32 + l32), 0);
 #pragma unroll
-        for (int i = 0; i < C::CH; ++i) rv[i] = row_of(tile * 64 + i * C::RPL + lane / C::CH);
+        for (int i = 0; i < C::CH; ++i) rv[i] = find.at(p.c, own(tile * 64 + i * C::RPL + lane / C::CH), 0);
       }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -313,7 +312,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     };
 
     int tile = wk;
-    if (!idle && tile < n_cache) fetch(tile);
+    if (!idle && tile < n_cache) look(tile), fetch(tile), look(tile + WK);
     bf16x8 q[C::NS];
     const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
 #pragma unroll
@@ -374,7 +373,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
             s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(kx[kb][st / 4][st % 4], sc), q[st], s[kb], 0, 0, 0);
           }
         const int left = n_keys - tile * 64;
-        if (tile + WK < n_cache) fetch(tile + WK);
+        if (tile + WK < n_cache) fetch(tile + WK), look(tile + 2 * WK);
         if (left < 64) {
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
@@ -592,7 +591,7 @@ int check_four(const tva_attn4_args *a, bool shapes_only) {
   if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
   if (a->plan_rows != 0 && a->plan_rows != 32 && a->plan_rows != 64 && a->plan_rows != 128) return TVA_INVALID_ARG;
   if (a->max_T > TVA_MAX_TREE) return TVA_UNSUPPORTED;
-  if (a->max_L > 0x7fffff00) return TVA_UNSUPPORTED;  // (positions are rounded up to whole tiles)
+  if (a->max_L > 1 << 29) return TVA_UNSUPPORTED;  // (page_of; positions are rounded up to whole tiles)
   if (shapes_only) return TVA_OK;
   if (!(a->scale > 0.f)) return TVA_INVALID_ARG;
   if (a->sum_T == 0) return TVA_OK;

@@ -23,22 +23,46 @@ struct CacheView {
   char *k, *v;
   char *k_row_scale, *v_row_scale;
   const int32_t *cu_L, *page_table;
-  int page_size, page_shift, max_pages;  // page_shift: log2 of the page size, or -1
+  int page_size, max_pages;
+  uint32_t page_magic, page_bits;  // division by the page size, of positions below 2^30: page_of
   int64_t stride_page, stride_tok, stride_head;
 };
+
+// t / page_size, exact for t below 2^30 (page_magic is 2^(31 + page_bits) / page_size rounded up, 2^page_bits >= page_size)
+__device__ __forceinline__ int page_of(const CacheView &c, int t) { return (int)(__umulhi((uint32_t)t * 2u, c.page_magic) >> c.page_bits); }
 
 // Where position t of sequence b begins, head 0, in units.  The position is within the sequence's room.
 __device__ __forceinline__ int64_t position_at(const CacheView &c, int b, int t) {
   if (c.page_table) {
-    const int pi = c.page_shift >= 0 ? t >> c.page_shift : t / c.page_size;
+    const int pi = page_of(c, t);
     const int page = c.page_table[(int64_t)b * c.max_pages + pi];
     return (int64_t)page * c.stride_page + (int64_t)(t - pi * c.page_size) * c.stride_tok;
   }
   return ((int64_t)c.cu_L[b] + t) * c.stride_tok;
 }
+
+// The same for one sequence and head, the look into the page table apart from what is made of it, so that a loop can look ahead:
+// entry() is what is read (nothing in the dense form), at() the place.
+template <bool PAGED>
+struct Finder {
+  const int32_t *table;
+  int64_t base;
+  __device__ __forceinline__ Finder(const CacheView &c, int b, int g) {
+    if constexpr (PAGED) table = c.page_table + (int64_t)b * c.max_pages, base = g * c.stride_head;
+    else table = nullptr, base = (int64_t)c.cu_L[b] * c.stride_tok + g * c.stride_head;
+  }
+  __device__ __forceinline__ int entry(const CacheView &c, int t) const {
+    if constexpr (PAGED) return table[page_of(c, t)];
+    else return 0;
+  }
+  __device__ __forceinline__ int64_t at(const CacheView &c, int t, int entry) const {
+    if constexpr (PAGED) return base + (int64_t)entry * c.stride_page + (int64_t)(t - page_of(c, t) * c.page_size) * c.stride_tok;
+    else return base + (int64_t)t * c.stride_tok;
+  }
+};
 // Positions of sequence b that have a place: what a call writes stays below it.
 __device__ __forceinline__ int64_t room_of(const CacheView &c, int b) {
-  return c.page_table ? (int64_t)c.max_pages * c.page_size : (int64_t)c.cu_L[b + 1] - c.cu_L[b];
+  return c.page_table ? min((int64_t)c.max_pages * c.page_size, (int64_t)1 << 30) : (int64_t)c.cu_L[b + 1] - c.cu_L[b];
 }
 
 // Checks a cache argument and turns it into a view: TVA_OK or a negative status.
@@ -52,6 +76,7 @@ inline int view_of(const tva_cache &a, int Hkv, int D, bool need_v, CacheView *c
   const bool dense = a.cu_L != nullptr, paged = a.page_table != nullptr;
   if (dense == paged) return TVA_INVALID_ARG;
   if (paged && (a.page_size <= 0 || a.max_pages <= 0)) return TVA_INVALID_ARG;
+  if (paged && a.page_size > 1 << 30) return TVA_UNSUPPORTED;
   if (a.stride_page < 0 || a.stride_tok < 0 || a.stride_head < 0) return TVA_INVALID_ARG;
   const int unit = four ? D : a.kind == TVA_ROWS_E4M3 ? 16 : 8;
   if (a.stride_page % unit || a.stride_tok % unit || a.stride_head % unit) return TVA_INVALID_ARG;
@@ -60,9 +85,9 @@ inline int view_of(const tva_cache &a, int Hkv, int D, bool need_v, CacheView *c
   c->k = (char *)a.k, c->v = (char *)a.v, c->k_row_scale = (char *)a.k_row_scale, c->v_row_scale = (char *)a.v_row_scale;
   c->cu_L = a.cu_L, c->page_table = a.page_table;
   c->page_size = paged ? a.page_size : 1, c->max_pages = a.max_pages;
-  c->page_shift = -1;
-  for (int s = 0; s < 31; ++s)
-    if (c->page_size == 1 << s) c->page_shift = s;
+  c->page_bits = 0;
+  while ((1u << c->page_bits) < (uint32_t)c->page_size) ++c->page_bits;
+  c->page_magic = (uint32_t)(((1ull << (31 + c->page_bits)) + (uint32_t)c->page_size - 1) / (uint32_t)c->page_size);
   c->stride_head = (a.stride_head ? a.stride_head : D) / per;
   c->stride_tok = (a.stride_tok ? a.stride_tok : (int64_t)Hkv * D) / per;
   c->stride_page = a.stride_page ? a.stride_page / per : (int64_t)c->page_size * c->stride_tok;

@@ -34,6 +34,7 @@ struct WeighParams {
   int32_t *pos;
   int64_t ld;
   int Hq, Hkv, G, max_rows, max_L;
+  int blocks;  // of 32 keys, per wave
   float scale_log2;
 };
 
@@ -49,64 +50,80 @@ __device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kWeighWaves = 4;
+constexpr int kWeighWaves = 4, kStayBlocks = 2;
 
-// Grid: KV head, 128 * KB keys, sequence.  Wave w has keys 32 KB w .. 32 KB (w + 1) - 1 of the workgroup's.
-template <int D, int KIND, int KB>
+// What a lane reads of a K row, as it lies in the cache: elements 16 s + 8 half of step s (bf16), or half of the row per lane half.
+template <int D, int KIND>
+struct RawK {
+  static constexpr int AHEAD = KIND == TVA_ROWS_BF16 ? 2 : KIND == TVA_ROWS_E4M3 ? 3 : 4;  // blocks on their way
+  static constexpr int NS = D / 16, N = KIND == TVA_ROWS_BF16 ? NS : KIND == TVA_ROWS_E4M3 ? NS / 2 : NS / 4;
+  u32x4 x[N];
+  uint32_t scale;
+  __device__ __forceinline__ void read(const CacheView &c, int64_t at, int half) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (KIND == TVA_ROWS_BF16) x[i] = *(const u32x4 *)(c.k + (at + i * 16 + half * 8) * 2);
+      else if constexpr (KIND == TVA_ROWS_E4M3) x[i] = *(const u32x4 *)(c.k + at + half * (D / 2) + i * 16);
+      else x[i] = *(const u32x4 *)(c.k + at * (D / 2) + half * (D / 4) + i * 16);
+    }
+    if constexpr (KIND == TVA_ROWS_E2M1) {
+      if constexpr (D == 128) scale = *(const uint16_t *)(c.k_row_scale + at * 4 + half * 2);
+      else scale = *(const uint8_t *)(c.k_row_scale + at * 2 + half);
+    }
+  }
+  __device__ __forceinline__ bf16x8 operand(int s) const {
+    if constexpr (KIND == TVA_ROWS_BF16) return __builtin_bit_cast(bf16x8, x[s]);
+    else if constexpr (KIND == TVA_ROWS_E4M3) return widen8_e4m3(u32x2{x[s / 2][s % 2 * 2], x[s / 2][s % 2 * 2 + 1]});
+    else return widen8(x[s / 4][s % 4], exponent_byte(s < 4 ? scale & 255 : scale >> 8));
+  }
+};
+
+// Grid: waves of a sequence (head fastest: the heads of a token lie side by side in a token-major cache, and a workgroup's waves read
+// whole lines of it), sequence.  A wave walks p.blocks blocks of 32 keys, the next block's rows on their way.
+// STAY: the query rows' operands (at most 64 rows) stay in registers; else they are read again for every block of keys.
+template <int D, int KIND, bool STAY, bool PAGED>
 __global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighParams p) {
   constexpr int NS = D / 16;
-  __shared__ __align__(16) float lds[kWeighWaves][2][32];
-  const int g = blockIdx.x, b = blockIdx.z;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  __shared__ __align__(16) float lds[kWeighWaves][kStayBlocks][2][32];
+  const int b = blockIdx.y;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int id = blockIdx.x * kWeighWaves + wave, g = id % p.Hkv;
+  const int key0 = (id / p.Hkv) * p.blocks * 32;
   const int t0 = p.cu_T[b], T = p.cu_T[b + 1] - t0;
   const int all = p.L[b], L = min(all, p.max_L);
   const int n = min(min(p.path ? p.path_len[b] : T, p.max_rows), all);
-  const int key0 = (blockIdx.y * kWeighWaves + wave) * (32 * KB);
+  const int end = min(L, key0 + p.blocks * 32);
   if (n <= 0 || key0 >= L) return;  // (no barriers below: a wave keeps to itself)
-
-  // ---- this lane's keys as operands: elements 16 s + 8 half of step s (bf16), or half of the row per lane half
-  bf16x8 k[KB][NS];
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb) {
-    const int64_t at = position_at(p.c, b, min(key0 + kb * 32 + l32, L - 1)) + g * p.c.stride_head;
-    if constexpr (KIND == TVA_ROWS_BF16) {
-#pragma unroll
-      for (int s = 0; s < NS; ++s) k[kb][s] = *(const bf16x8 *)(p.c.k + (at + s * 16 + half * 8) * 2);
-    } else if constexpr (KIND == TVA_ROWS_E4M3) {
-      u32x4 x[NS / 2];
-#pragma unroll
-      for (int s = 0; s < NS / 2; ++s) x[s] = *(const u32x4 *)(p.c.k + at + half * (D / 2) + s * 16);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) k[kb][s] = widen8_e4m3(u32x2{x[s / 2][s % 2 * 2], x[s / 2][s % 2 * 2 + 1]});
-    } else {
-      u32x4 x[NS / 4];
-#pragma unroll
-      for (int s = 0; s < NS / 4; ++s) x[s] = *(const u32x4 *)(p.c.k + at * (D / 2) + half * (D / 4) + s * 16);
-      uint32_t sc;
-      if constexpr (D == 128) sc = *(const uint16_t *)(p.c.k_row_scale + at * 4 + half * 2);
-      else sc = *(const uint8_t *)(p.c.k_row_scale + at * 2 + half);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) k[kb][s] = widen8(x[s / 4][s % 4], exponent_byte(s < 4 ? sc & 255 : sc >> 8));
-    }
-  }
-
-  float sum[KB];
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb) sum[kb] = 0.f;
+  const Finder<PAGED> find(p.c, b, g);
+  auto own = [&](int key) __attribute__((always_inline)) { return min(key + l32, L - 1); };
+  constexpr int AHEAD = RawK<D, KIND>::AHEAD;
+  // Loads return in the order they were asked for: what a block needs (its weights too) is asked for AHEAD blocks earlier, or waiting
+  // for it would wait for all that was asked for since.
   const int old = all - n;  // positions below it are seen by every row
-  const bool all_seen = key0 + 32 * KB <= old;
+  float *const weight = p.weight + ((int64_t)b * p.Hkv + g) * p.ld;
+  RawK<D, KIND> raw[AHEAD];
+  float before[AHEAD];
+  int entry[AHEAD];  // the page of this lane's key, looked up 2 AHEAD blocks earlier
+  auto ask = [&](int u, int key) __attribute__((always_inline)) {
+    raw[u].read(p.c, find.at(p.c, own(key), entry[u]), half);
+    before[u] = weight[own(key)];
+  };
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) entry[u] = find.entry(p.c, own(key0 + 32 * u));
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) ask(u, key0 + 32 * u);
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) entry[u] = find.entry(p.c, own(key0 + 32 * (AHEAD + u)));
+
   const int R = n * p.G;
-  float *lrow = lds[wave][0];
-  int *seen_to = (int *)lds[wave][1];
-  for (int r0 = 0; r0 < R; r0 += 32) {
-    // rows r0 .. r0+31: query operand (a row per lane), log-sum-exp and last seen position
+  // rows r0 .. r0+31: query operand (a row per lane), and in LDS minus log-sum-exp and the last position the row saw
+  auto rows_of = [&](int r0, bf16x8 (&q)[NS], float (&to)[2][32]) __attribute__((always_inline)) {
     const int r = min(r0 + l32, R - 1), i = r / p.G, head = g * p.G + (r - i * p.G);
     const int node = p.path ? p.path[(int64_t)b * p.max_rows + i] : i;
     const bool there = node >= 0 && node < T;
     const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
     const float lse = p.lse[row];
     const bool counts = there && r0 + l32 < R && lse != -INFINITY;
-    bf16x8 q[NS];
     const __bf16 *from = p.q + row * D;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -114,39 +131,62 @@ __global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighPara
       if (!counts) q[s] = bf16x8{};  // (whatever it holds)
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (half == 0) lrow[l32] = counts ? -lse * kLog2e : -INFINITY, seen_to[l32] = old + i;
+    if (half == 0) to[0][l32] = counts ? -lse * kLog2e : -INFINITY, to[1][l32] = __int_as_float(old + i);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    f32x16 x[KB];
+  };
+  // a block's products with a block of rows, as weights, added to this lane's key's sum (of this half's rows)
+  auto weigh = [&](const bf16x8 (&k)[NS], const bf16x8 (&q)[NS], const float (&to)[2][32], int key, bool all_seen, float &sum) __attribute__((always_inline)) {
+    f32x16 x = {};
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) x[kb] = f32x16{};
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[kb][s], x[kb], 0, 0, 0);
+    for (int s = 0; s < NS; ++s) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[s], x, 0, 0, 0);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const f32x4 l = *(const f32x4 *)(lrow + 8 * c + 4 * half);
-      typedef int i32x4 __attribute__((ext_vector_type(4)));
-      i32x4 to = {};
-      if (!all_seen) to = *(const i32x4 *)(seen_to + 8 * c + 4 * half);
+      const f32x4 l = *(const f32x4 *)(to[0] + 8 * c + 4 * half);
+      f32x4 last = {};
+      if (!all_seen) last = *(const f32x4 *)(to[1] + 8 * c + 4 * half);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(x[kb][c * 4 + e], p.scale_log2, l[e]));
-          sum[kb] += all_seen || key0 + kb * 32 + l32 <= to[e] ? w : 0.f;
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(x[c * 4 + e], p.scale_log2, l[e]));
+        sum += all_seen || key + l32 <= __float_as_int(last[e]) ? w : 0.f;
+      }
     }
+  };
+
+  bf16x8 q[STAY ? kStayBlocks : 1][NS];
+  if constexpr (STAY) {
+    rows_of(0, q[0], lds[wave][0]);
+    if (R > 32) rows_of(32, q[1], lds[wave][1]);
   }
+  for (int base = key0; base < end; base += 32 * AHEAD)
 #pragma unroll
-  for (int kb = 0; kb < KB; ++kb) {
-    const float w = half_sum(sum[kb]);
-    const int t = key0 + kb * 32 + l32;
-    const int64_t at = ((int64_t)b * p.Hkv + g) * p.ld + t;
-    if (half || t >= L) continue;
-    p.weight[at] = (t < old ? p.weight[at] : 0.f) + w;
-    if (p.pos && t >= old) p.pos[at] = p.first_pos[b] + (t - old);
-  }
+    for (int u = 0; u < AHEAD; ++u) {
+      const int key = base + 32 * u;
+      if (key >= end) break;
+      const int t = key + l32;
+      bf16x8 k[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[s] = raw[u].operand(s);
+      const bool all_seen = key + 32 <= old;
+      float sum = 0.f;
+      if constexpr (STAY) {
+        weigh(k, q[0], lds[wave][0], key, all_seen, sum);
+        if (R > 32) weigh(k, q[1], lds[wave][1], key, all_seen, sum);
+      } else {
+        for (int r0 = 0; r0 < R; r0 += 32) {
+          rows_of(r0, q[0], lds[wave][0]);
+          weigh(k, q[0], lds[wave][0], key, all_seen, sum);
+        }
+      }
+      const float w = half_sum(sum) + (t < old ? before[u] : 0.f);
+      if (key + 32 * AHEAD < end) {
+        ask(u, key + 32 * AHEAD);
+        entry[u] = find.entry(p.c, own(key + 64 * AHEAD));
+      }
+      if (!half && t < L) {
+        weight[t] = w;
+        if (p.pos && t >= old) p.pos[((int64_t)b * p.Hkv + g) * p.ld + t] = p.first_pos[b] + (t - old);
+      }
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -229,28 +269,43 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   if (n == 0) return;
   const int newest = p.newest ? p.newest[b] : 0x7fffffff;
   const bool ages = p.newest != nullptr;
-  auto key_at = [&](int t) __attribute__((always_inline)) {
-    const int age = pos ? pos[t] : t;
-    return key_of(p, weight[t], t < p.n_first || (ages && age >= newest));
+  // Slots from L on count as the smallest key there is: they come last among equals, behind all that n < L can reach.
+  // Reads are batched, ROUNDS of the workgroup at a time (one by one each waits for the one before: 512 rows of up to 32768 slots with
+  // ages 164 us instead of 60).
+  constexpr int ROUNDS = ITEMS > 0 && ITEMS < 8 ? ITEMS : 8;
+  auto read = [&](int t0, uint32_t (&k)[ROUNDS]) __attribute__((always_inline)) {
+    float w[ROUNDS];
+    int age[ROUNDS];
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) w[i] = weight[min(t0 + i * kChooseThreads, L - 1)];
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) age[i] = pos ? pos[min(t0 + i * kChooseThreads, L - 1)] : t0 + i * kChooseThreads;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      const int t = t0 + i * kChooseThreads;
+      k[i] = t < L ? key_of(p, w[i], t < p.n_first || (ages && age[i] >= newest)) : 0;
+    }
   };
   uint32_t keys[ITEMS > 0 ? ITEMS : 1];
   if constexpr (ITEMS > 0) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int t = i * kChooseThreads + tid;
-      keys[i] = t < L ? key_at(t) : 0;
+    for (int i = 0; i < ITEMS; i += ROUNDS) {
+      uint32_t k[ROUNDS];
+      read(i * kChooseThreads + tid, k);
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) keys[i + j] = k[j];
     }
   }
-  const int rounds = (L + kChooseThreads - 1) / kChooseThreads;
   auto each = [&](auto use) __attribute__((always_inline)) {
     if constexpr (ITEMS > 0) {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
-        if (i < rounds) use(i * kChooseThreads + tid, keys[i]);
+      for (int i = 0; i < ITEMS; ++i) use(i * kChooseThreads + tid, keys[i]);
     } else {
-      for (int i = 0; i < rounds; ++i) {
-        const int t = i * kChooseThreads + tid;
-        use(t, t < L ? key_at(t) : 0u);
+      for (int t = tid; t - tid < L; t += ROUNDS * kChooseThreads) {
+        uint32_t k[ROUNDS];
+        read(t, k);
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) use(t + i * kChooseThreads, k[i]);
       }
     }
   };
@@ -261,8 +316,8 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = tid; i < 256 * kCopies; i += kChooseThreads) hist[i] = 0;
     __syncthreads();
-    each([&](int t, uint32_t k) __attribute__((always_inline)) {
-      if (t < L && (shift == 24 || (k ^ prefix) >> (shift + 8) == 0)) atomicAdd(&hist[((k >> shift) & 255) * kCopies + (lane & (kCopies - 1))], 1);
+    each([&](int, uint32_t k) __attribute__((always_inline)) {
+      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[((k >> shift) & 255) * kCopies + (lane & (kCopies - 1))], 1);
     });
     __syncthreads();
     int mine = 0;
@@ -279,7 +334,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   }
   // ---- a bit per slot: above the n-th key, equal to it (want of those stay, the lowest)
   each([&](int t, uint32_t k) __attribute__((always_inline)) {
-    const uint64_t a = __ballot(t < L && k > prefix), e = __ballot(t < L && k == prefix);
+    const uint64_t a = __ballot(k > prefix), e = __ballot(k == prefix);
     if (lane == 0 && (t >> 6) < p.words) above[t >> 6] = a, equal[t >> 6] = e;
   });
   __syncthreads();
@@ -420,12 +475,25 @@ int tva_key_weights(const tva_key_weight_args *a, void *stream) {
   p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.max_rows = a->max_rows, p.max_L = a->max_L;
   const float ks = a->cache.kind == TVA_ROWS_E4M3 && a->cache.k_scale != 0.f ? a->cache.k_scale : 1.f;
   p.scale_log2 = a->scale * ks * kLog2e;
-  const int64_t blocks = ((int64_t)a->max_L + 128 - 1) / 128;
-  if (a->B > 65535 || blocks > 65535) return TVA_UNSUPPORTED;
+  // blocks per wave: as many as leave 4096 waves (half of what the chip holds), at most 16
+  const int64_t all_blocks = ((int64_t)a->max_L + 31) / 32;
+  p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(16, all_blocks * a->B * a->Hkv / 4096));
+  const int64_t waves = (all_blocks + p.blocks - 1) / p.blocks * a->Hkv, groups = (waves + kWeighWaves - 1) / kWeighWaves;
+  if (a->B > 65535 || groups > 0x7fffffff || a->max_L > 1 << 29) return TVA_UNSUPPORTED;
+  const bool stay = (int64_t)a->max_rows * p.G <= 32 * kStayBlocks;
   (void)hipGetLastError();
   return by_kind(a->D, a->cache.kind, [&](auto d, auto kind) {
-    hipLaunchKernelGGL((weigh_kernel<decltype(d)::value, decltype(kind)::value, 1>), dim3(a->Hkv, (unsigned)blocks, a->B), dim3(64 * kWeighWaves), 0,
-                       (hipStream_t)stream, p);
+    constexpr int D = decltype(d)::value, KIND = decltype(kind)::value;
+    const dim3 grid((unsigned)groups, a->B), block(64 * kWeighWaves);
+    auto launch = [&](auto st, auto pg) {
+      hipLaunchKernelGGL((weigh_kernel<D, KIND, decltype(st)::value, decltype(pg)::value>), grid, block, 0, (hipStream_t)stream, p);
+    };
+    auto form = [&](auto st) {
+      if (a->cache.page_table) launch(st, std::true_type{});
+      else launch(st, std::false_type{});
+    };
+    if (stay) form(std::true_type{});
+    else form(std::false_type{});
   });
 }
 size_t tva_sizeof_key_weight_args(void) { return sizeof(tva_key_weight_args); }
@@ -448,6 +516,7 @@ int tva_evict_select(const tva_evict_select_args *a, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
   if (a->max_L <= 4 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<4>, grid, block, bytes, st, p);
+  else if (a->max_L <= 16 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<16>, grid, block, bytes, st, p);
   else if (a->max_L <= 32 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<32>, grid, block, bytes, st, p);
   else hipLaunchKernelGGL(choose_kernel<0>, grid, block, bytes, st, p);
   return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
