@@ -50,12 +50,12 @@ __device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kWeighWaves = 4, kStayBlocks = 2;
+constexpr int kWeighWaves = 4;
 
 // What a lane reads of a K row, as it lies in the cache: elements 16 s + 8 half of step s (bf16), or half of the row per lane half.
 template <int D, int KIND>
 struct RawK {
-  static constexpr int AHEAD = KIND == TVA_ROWS_BF16 ? 2 : KIND == TVA_ROWS_E4M3 ? 3 : 4;  // blocks on their way
+  static constexpr int AHEAD = KIND == TVA_ROWS_BF16 ? 1 : KIND == TVA_ROWS_E4M3 ? 2 : 3;  // blocks on their way
   static constexpr int NS = D / 16, N = KIND == TVA_ROWS_BF16 ? NS : KIND == TVA_ROWS_E4M3 ? NS / 2 : NS / 4;
   u32x4 x[N];
   uint32_t scale;
@@ -80,11 +80,11 @@ struct RawK {
 
 // Grid: waves of a sequence (head fastest: the heads of a token lie side by side in a token-major cache, and a workgroup's waves read
 // whole lines of it), sequence.  A wave walks p.blocks blocks of 32 keys, the next block's rows on their way.
-// STAY: the query rows' operands (at most 64 rows) stay in registers; else they are read again for every block of keys.
-template <int D, int KIND, bool STAY, bool PAGED>
-__global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighParams p) {
+// The operands of the first 32 query rows (all there are, mostly) stay in registers; further ones are read again for every block of keys.
+template <int D, int KIND, bool PAGED>
+__global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS_BF16 ? 3 : 4) weigh_kernel(const WeighParams p) {
   constexpr int NS = D / 16;
-  __shared__ __align__(16) float lds[kWeighWaves][kStayBlocks][2][32];
+  __shared__ __align__(16) float lds[kWeighWaves][2][2][32];  // of the rows that stay, and of others
   const int b = blockIdx.y;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int id = blockIdx.x * kWeighWaves + wave, g = id % p.Hkv;
@@ -152,11 +152,8 @@ __global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighPara
     }
   };
 
-  bf16x8 q[STAY ? kStayBlocks : 1][NS];
-  if constexpr (STAY) {
-    rows_of(0, q[0], lds[wave][0]);
-    if (R > 32) rows_of(32, q[1], lds[wave][1]);
-  }
+  bf16x8 q[NS];
+  rows_of(0, q, lds[wave][0]);
   for (int base = key0; base < end; base += 32 * AHEAD)
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
@@ -168,14 +165,11 @@ __global__ void __launch_bounds__(64 * kWeighWaves) weigh_kernel(const WeighPara
       for (int s = 0; s < NS; ++s) k[s] = raw[u].operand(s);
       const bool all_seen = key + 32 <= old;
       float sum = 0.f;
-      if constexpr (STAY) {
-        weigh(k, q[0], lds[wave][0], key, all_seen, sum);
-        if (R > 32) weigh(k, q[1], lds[wave][1], key, all_seen, sum);
-      } else {
-        for (int r0 = 0; r0 < R; r0 += 32) {
-          rows_of(r0, q[0], lds[wave][0]);
-          weigh(k, q[0], lds[wave][0], key, all_seen, sum);
-        }
+      weigh(k, q, lds[wave][0], key, all_seen, sum);
+      for (int r0 = 32; r0 < R; r0 += 32) {
+        bf16x8 more[NS];
+        rows_of(r0, more, lds[wave][1]);
+        weigh(k, more, lds[wave][1], key, all_seen, sum);
       }
       const float w = half_sum(sum) + (t < old ? before[u] : 0.f);
       if (key + 32 * AHEAD < end) {
@@ -480,20 +474,12 @@ int tva_key_weights(const tva_key_weight_args *a, void *stream) {
   p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(16, all_blocks * a->B * a->Hkv / 4096));
   const int64_t waves = (all_blocks + p.blocks - 1) / p.blocks * a->Hkv, groups = (waves + kWeighWaves - 1) / kWeighWaves;
   if (a->B > 65535 || groups > 0x7fffffff || a->max_L > 1 << 29) return TVA_UNSUPPORTED;
-  const bool stay = (int64_t)a->max_rows * p.G <= 32 * kStayBlocks;
   (void)hipGetLastError();
   return by_kind(a->D, a->cache.kind, [&](auto d, auto kind) {
     constexpr int D = decltype(d)::value, KIND = decltype(kind)::value;
     const dim3 grid((unsigned)groups, a->B), block(64 * kWeighWaves);
-    auto launch = [&](auto st, auto pg) {
-      hipLaunchKernelGGL((weigh_kernel<D, KIND, decltype(st)::value, decltype(pg)::value>), grid, block, 0, (hipStream_t)stream, p);
-    };
-    auto form = [&](auto st) {
-      if (a->cache.page_table) launch(st, std::true_type{});
-      else launch(st, std::false_type{});
-    };
-    if (stay) form(std::true_type{});
-    else form(std::false_type{});
+    if (a->cache.page_table) hipLaunchKernelGGL((weigh_kernel<D, KIND, true>), grid, block, 0, (hipStream_t)stream, p);
+    else hipLaunchKernelGGL((weigh_kernel<D, KIND, false>), grid, block, 0, (hipStream_t)stream, p);
   });
 }
 size_t tva_sizeof_key_weight_args(void) { return sizeof(tva_key_weight_args); }
