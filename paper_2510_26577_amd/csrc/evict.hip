@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
   const int end = min(L, key0 + p.blocks * 32);
   if (n <= 0 || key0 >= L) return;  // (no barriers below: a wave keeps to itself)
   const Finder<PAGED> find(p.c, b, g);
-  auto own = [&](int key) __attribute__((always_inline)) { return min(key + l32, L - 1); };
+  auto own = [&](int key) __attribute__((always_inline)) { return min(key + l32, end - 1); };  // past the end: the last row
   constexpr int AHEAD = RawK<D, KIND>::AHEAD;
-  // Loads return in the order they were asked for: what a block needs (its weights too) is asked for AHEAD blocks earlier, or waiting
-  // for it would wait for all that was asked for since.
+  // Loads return in the order they were asked for, and a wait is a count of those behind the one waited for: what a block needs (its
+  // weights too) is asked for AHEAD blocks earlier, and always, so that the counts are known.
   const int old = all - n;  // positions below it are seen by every row
   float *const weight = p.weight + ((int64_t)b * p.Hkv + g) * p.ld;
   RawK<D, KIND> raw[AHEAD];
@@ -154,11 +154,11 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
 
   bf16x8 q[NS];
   rows_of(0, q, lds[wave][0]);
-  for (int base = key0; base < end; base += 32 * AHEAD)
+  const int first_pos = p.pos && end > old ? p.first_pos[b] : 0;
+  for (int base = key0;; base += 32 * AHEAD)
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int key = base + 32 * u;
-      if (key >= end) break;
       const int t = key + l32;
       bf16x8 k[NS];
 #pragma unroll
@@ -172,14 +172,13 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
         weigh(k, more, lds[wave][1], key, all_seen, sum);
       }
       const float w = half_sum(sum) + (t < old ? before[u] : 0.f);
-      if (key + 32 * AHEAD < end) {
-        ask(u, key + 32 * AHEAD);
-        entry[u] = find.entry(p.c, own(key + 64 * AHEAD));
-      }
-      if (!half && t < L) {
+      ask(u, key + 32 * AHEAD);
+      entry[u] = find.entry(p.c, own(key + 64 * AHEAD));
+      if (!half && t < end) {
         weight[t] = w;
-        if (p.pos && t >= old) p.pos[((int64_t)b * p.Hkv + g) * p.ld + t] = p.first_pos[b] + (t - old);
+        if (p.pos && t >= old) p.pos[((int64_t)b * p.Hkv + g) * p.ld + t] = first_pos + (t - old);
       }
+      if (key + 32 >= end) return;
     }
 }
 
@@ -265,7 +264,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   const bool ages = p.newest != nullptr;
   // Slots from L on count as the smallest key there is: they come last among equals, behind all that n < L can reach.
   // Reads are batched, ROUNDS of the workgroup at a time (one by one each waits for the one before: 512 rows of up to 32768 slots with
-  // ages 164 us instead of 60).
+  // ages 164 us instead of 114).
   constexpr int ROUNDS = ITEMS > 0 && ITEMS < 8 ? ITEMS : 8;
   auto read = [&](int t0, uint32_t (&k)[ROUNDS]) __attribute__((always_inline)) {
     float w[ROUNDS];
@@ -469,9 +468,9 @@ int tva_key_weights(const tva_key_weight_args *a, void *stream) {
   p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.max_rows = a->max_rows, p.max_L = a->max_L;
   const float ks = a->cache.kind == TVA_ROWS_E4M3 && a->cache.k_scale != 0.f ? a->cache.k_scale : 1.f;
   p.scale_log2 = a->scale * ks * kLog2e;
-  // blocks per wave: as many as leave 4096 waves (half of what the chip holds), at most 16
+  // blocks per wave: as many as leave 4096 waves, at most 8 (16 x 16384 .. 32768 4-bit keys: with 4 / 8 / 16 / 32 79 / 70.6 / 71.9 / 86 us)
   const int64_t all_blocks = ((int64_t)a->max_L + 31) / 32;
-  p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(16, all_blocks * a->B * a->Hkv / 4096));
+  p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, all_blocks * a->B * a->Hkv / 4096));
   const int64_t waves = (all_blocks + p.blocks - 1) / p.blocks * a->Hkv, groups = (waves + kWeighWaves - 1) / kWeighWaves;
   if (a->B > 65535 || groups > 0x7fffffff || a->max_L > 1 << 29) return TVA_UNSUPPORTED;
   (void)hipGetLastError();
