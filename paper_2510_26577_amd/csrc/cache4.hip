@@ -38,7 +38,7 @@ struct RowsParams {
   uint16_t *k_rows, *v_rows;
   CacheView c;
   int32_t *L_out, *err_flag;
-  int Hkv, max_rows;
+  int Hkv, max_rows, n_layers;
   int64_t layer_rows;   // elements of k_rows / v_rows between layers
   int64_t layer_cache;  // rows of the cache between layers
 };
@@ -59,80 +59,136 @@ __device__ __forceinline__ bool find_row(const RowsParams &p, int b, int j, int 
   return true;
 }
 
-// |x| bits of the largest finite of eight bf16 numbers
-__device__ __forceinline__ uint32_t largest(const u16x8 x) {
-  uint32_t a = 0;
+// |x| bits of the largest finite of eight bf16 numbers, and whether all are finite
+__device__ __forceinline__ uint32_t largest(const u16x8 x, bool *finite) {
+  uint32_t a = 0, all = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t m = x[i] & 0x7fff;
     a = m < 0x7f80 && m > a ? m : a;
+    all = max(all, m);
   }
+  *finite = all < 0x7f80;
   return a;
 }
-// Code of x / s: s times the borders between codes is exact (s has at most 4 significant bits, a border 3), and so are the
-// comparisons.  NaN compares false: 0.
+// Code of x / s by the borders between codes: s (at most 4 significant bits) times a border (3) is exact, and so are the comparisons.
+// NaN compares false: 0.
 __device__ __forceinline__ uint32_t code_of(float x, float s) {
   const float a = fabsf(x);
   const uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) + (a >= 3.5f * s) + (a > 5.f * s);
   return c | (a == a ? (__float_as_uint(x) >> 28) & 8u : 0u);
 }
-__device__ __forceinline__ uint32_t codes_of(const u16x8 x, float s) {
+__device__ uint32_t codes_of(const u16x8 x, float s) {
   uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) w |= code_of(__uint_as_float((uint32_t)x[i] << 16), s) << (4 * i);
   return w;
 }
+// The same by the conversion instructions, for finite x of at most 6 s: they divide by a power of two and round to nearest even.
+__device__ __forceinline__ uint32_t codes_k(const u16x8 x, float s) {
+  uint32_t w = 0;
+#define PAIR(i) bf16x2{__builtin_bit_cast(__bf16, (uint16_t)x[2 * i]), __builtin_bit_cast(__bf16, (uint16_t)x[2 * i + 1])}
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(0), s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(1), s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(2), s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(3), s, 3);
+#undef PAIR
+  return w;
+}
+// V's scale is no power of two: the quotient comes from a reciprocal and one correction, exact where it is a border (only equality
+// with one is near enough to matter: x has 8 bits and s times a border 7).
+__device__ __forceinline__ uint32_t codes_v(const u16x8 x, float s) {
+  const float r = 1.f / s;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = __uint_as_float((uint32_t)x[i] << 16), q = a * r;
+    y[i] = fmaf(fmaf(-q, s, a), r, q);
+  }
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.f, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.f, 3);
+  return w;
+}
+
+// Layers that a workgroup takes its rows of at once: what leads to a row (lengths, path, page) is read once for them.
+constexpr int kRowLayers = 4;
 
 template <int D>
 __global__ void __launch_bounds__(256) store_rows_kernel(const RowsParams p) {
   constexpr int LPR = D / 8;  // lanes per row
-  const int b = blockIdx.y, layer = blockIdx.z;
+  const int b = blockIdx.y, layer0 = blockIdx.z * kRowLayers, here = min(p.n_layers - layer0, kRowLayers);
   const int idx = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, part = threadIdx.x % LPR;
   const int j = idx / p.Hkv, g = idx - j * p.Hkv;
-  if (idx == 0 && part == 0 && layer == 0 && p.L_out) {
+  if (idx == 0 && part == 0 && layer0 == 0 && p.L_out) {
     const int n = p.path ? p.path_len[b] : p.cu_T[b + 1] - p.cu_T[b];
     p.L_out[b] = p.L[b] + (n < p.max_rows ? n : p.max_rows);
   }
   int64_t from, to;
   if (!find_row(p, b, j, g, &from, &to)) return;  // (the lanes of a row leave together)
-  to += layer * p.layer_cache;
-  const int64_t e = layer * p.layer_rows + (from * p.Hkv + g) * D + part * 8;
-  const u16x8 k = *(const u16x8 *)(p.k_rows + e), v = *(const u16x8 *)(p.v_rows + e);
-  uint32_t ak = largest(k), av = largest(v);
+  to += layer0 * p.layer_cache;
+  const int64_t e = layer0 * p.layer_rows + (from * p.Hkv + g) * D + part * 8;
+  u16x8 ks[kRowLayers], vs[kRowLayers];
 #pragma unroll
-  for (int o = 1; o < LPR; o *= 2) {
-    if (o < 4) ak = max(ak, (uint32_t)__shfl_xor((int)ak, o));
-    av = max(av, (uint32_t)__shfl_xor((int)av, o));
+  for (int l = 0; l < kRowLayers; ++l) {
+    const int64_t at = e + min(l, here - 1) * p.layer_rows;
+    ks[l] = *(const u16x8 *)(p.k_rows + at), vs[l] = *(const u16x8 *)(p.v_rows + at);
   }
-  // K: a = (1 + m/128) 2^(E-127) <= 6 * 2^e
-  const int ek = min(max((int)(ak >> 7) - 127 - ((ak & 127) > 64 ? 1 : 2), -96), 124);
-  // V: a = n/256 * 2^(E-126), the quotient by 6 rounded up to four bits
-  const int n = 128 + (int)(av & 127), ev = (int)(av >> 7) - 126;
-  const float sv = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), ev - 7) : ldexpf((float)((n + 23) / 24), ev - 6), 0x1p-96f), 0x1p124f);
-  ((uint32_t *)p.c.k)[to * LPR + part] = codes_of(k, exponent_byte((uint32_t)(ek + 127)));
-  ((uint32_t *)p.c.v)[to * LPR + part] = codes_of(v, sv);
-  if (part % 4 == 0) ((uint8_t *)p.c.k_row_scale)[to * (D / 32) + part / 4] = (uint8_t)(ek + 127);
-  if (part == 0) ((uint16_t *)p.c.v_row_scale)[to] = (uint16_t)(__float_as_uint(sv) >> 16);
+#pragma unroll
+  for (int l = 0; l < kRowLayers; ++l, to += p.layer_cache) {
+    if (l >= here) return;
+    const u16x8 k = ks[l], v = vs[l];
+    bool fk, fv;
+    uint32_t ak = largest(k, &fk), av = largest(v, &fv);
+#pragma unroll
+    for (int o = 1; o < LPR; o *= 2) {
+      if (o < 4) ak = max(ak, (uint32_t)__shfl_xor((int)ak, o));
+      av = max(av, (uint32_t)__shfl_xor((int)av, o));
+    }
+    // K: a = (1 + m/128) 2^(E-127) <= 6 * 2^e
+    const int ek = (int)(ak >> 7) - 127 - ((ak & 127) > 64 ? 1 : 2), e2 = min(max(ek, -96), 124);
+    // V: a = n/256 * 2^(E-126), the quotient by 6 rounded up to four bits
+    const int n = 128 + (int)(av & 127), ev = (int)(av >> 7) - 126;
+    const float sv = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), ev - 7) : ldexpf((float)((n + 23) / 24), ev - 6), 0x1p-96f), 0x1p124f);
+    const float sk = exponent_byte((uint32_t)(e2 + 127));
+    const bool plain = fk && fv && ek == e2 && sv > 0x1p-96f && sv < 0x1p124f;  // (else: what the instructions would do is not asked)
+    uint32_t wk = codes_k(k, sk), wv = codes_v(v, sv);
+    if (!plain) wk = codes_of(k, sk), wv = codes_of(v, sv);
+    ((uint32_t *)p.c.k)[to * LPR + part] = wk;
+    ((uint32_t *)p.c.v)[to * LPR + part] = wv;
+    if (part % 4 == 0) ((uint8_t *)p.c.k_row_scale)[to * (D / 32) + part / 4] = (uint8_t)(e2 + 127);
+    if (part == 0) ((uint16_t *)p.c.v_row_scale)[to] = (uint16_t)(__float_as_uint(sv) >> 16);
+  }
 }
 
 template <int D>
 __global__ void __launch_bounds__(256) load_rows_kernel(const RowsParams p) {
   constexpr int LPR = D / 8;
-  const int b = blockIdx.y, layer = blockIdx.z;
+  const int b = blockIdx.y, layer0 = blockIdx.z * kRowLayers, here = min(p.n_layers - layer0, kRowLayers);
   const int idx = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, part = threadIdx.x % LPR;
   const int j = idx / p.Hkv, g = idx - j * p.Hkv;
   int64_t to, from;
   if (!find_row(p, b, j, g, &to, &from)) return;
-  from += layer * p.layer_cache;
-  const int64_t e = layer * p.layer_rows + (to * p.Hkv + g) * D + part * 8;
-  const uint32_t k = ((const uint32_t *)p.c.k)[from * LPR + part], v = ((const uint32_t *)p.c.v)[from * LPR + part];
-  const float sk = exponent_byte(((const uint8_t *)p.c.k_row_scale)[from * (D / 32) + part / 4]);
-  const float sv = __uint_as_float((uint32_t)((const uint16_t *)p.c.v_row_scale)[from] << 16);
-  *(bf16x8 *)(p.k_rows + e) = widen8(k, sk);
-  bf16x8 x = widen8(v, 1.f);
+  from += layer0 * p.layer_cache;
+  const int64_t e = layer0 * p.layer_rows + (to * p.Hkv + g) * D + part * 8;
+  uint32_t k[kRowLayers], v[kRowLayers], sk[kRowLayers], sv[kRowLayers];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (__bf16)((float)x[i] * sv);  // (at most 6 bits: exact)
-  *(bf16x8 *)(p.v_rows + e) = x;
+  for (int l = 0; l < kRowLayers; ++l) {
+    const int64_t at = from + min(l, here - 1) * p.layer_cache;
+    k[l] = ((const uint32_t *)p.c.k)[at * LPR + part], v[l] = ((const uint32_t *)p.c.v)[at * LPR + part];
+    sk[l] = ((const uint8_t *)p.c.k_row_scale)[at * (D / 32) + part / 4], sv[l] = ((const uint16_t *)p.c.v_row_scale)[at];
+  }
+#pragma unroll
+  for (int l = 0; l < kRowLayers; ++l) {
+    if (l >= here) return;
+    *(bf16x8 *)(p.k_rows + e + l * p.layer_rows) = widen8(k[l], exponent_byte(sk[l]));
+    bf16x8 x = widen8(v[l], 1.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (__bf16)((float)x[i] * __uint_as_float(sv[l] << 16));  // (at most 6 bits: exact)
+    *(bf16x8 *)(p.v_rows + e + l * p.layer_rows) = x;
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -610,7 +666,7 @@ template <int D>
 int launch_rows(const RowsParams &p, int B, int layers, bool load, hipStream_t st) {
   const int64_t groups = ((int64_t)p.max_rows * p.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8));
   if (groups > 0x7fffffff) return TVA_UNSUPPORTED;
-  const dim3 grid((unsigned)groups, B, layers);
+  const dim3 grid((unsigned)groups, B, (layers + kRowLayers - 1) / kRowLayers);
   if (load) hipLaunchKernelGGL(load_rows_kernel<D>, grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL(store_rows_kernel<D>, grid, dim3(256), 0, st, p);
   return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
@@ -633,7 +689,7 @@ int run_rows(const tva_rows_args *a, bool load, void *stream) {
   if (a->max_rows == 0) return TVA_OK;
   p.cu_T = a->cu_T, p.L = a->L, p.path = a->path, p.path_len = a->path_len;
   p.k_rows = (uint16_t *)a->k_rows, p.v_rows = (uint16_t *)a->v_rows;
-  p.L_out = a->L_out, p.err_flag = a->err_flag, p.Hkv = a->Hkv, p.max_rows = a->max_rows;
+  p.L_out = a->L_out, p.err_flag = a->err_flag, p.Hkv = a->Hkv, p.max_rows = a->max_rows, p.n_layers = layers;
   p.layer_rows = a->layer_stride_rows, p.layer_cache = a->layer_stride_cache / a->D;
   (void)hipGetLastError();
   return a->D == 128 ? launch_rows<128>(p, a->B, layers, load, (hipStream_t)stream) : launch_rows<64>(p, a->B, layers, load, (hipStream_t)stream);
