@@ -190,7 +190,7 @@ struct ChooseParams {
   const float *weight;
   int32_t *src, *L_out;
   int64_t ld, ld_src;
-  int B, H, max_L, n_first, words;  // words: 64-slot words of the longest row
+  int B, H, max_L, n_first, words, list;  // words: 64-slot words of the longest row; list: gaps listed at a time
 };
 
 constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kCopies = 16;
@@ -244,9 +244,10 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   uint64_t *above = (uint64_t *)lds, *equal = above + p.words;  // a bit per slot; above becomes the kept set
   uint64_t *part64 = equal + p.words;                            // kChooseWaves
   int *before = (int *)(part64 + kChooseWaves);                  // gaps before each word
-  int *rank0 = before + p.words;                                 // kept slots from n on before each word
+  int *rank0 = before + p.words + 1;                             // kept slots from n on before each word
   int *hist = rank0 + p.words;                                   // [256][kCopies]
   int *part = hist + 256 * kCopies;                              // kChooseWaves, and what a pass finds
+  int *list = part + 32;                                         // gaps by rank, p.list of them
   const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int L = min(max(p.L[b], 0), p.max_L), n = (int)min((int64_t)min(max(p.keep[b], 0), L), p.ld_src);
@@ -350,29 +351,33 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
     const uint64_t sums = scan_threads(mine, part64, &all) - mine;
     if (w < words) above[w] = kept, before[w] = gaps + (int)sums, rank0[w] = late + (int)(sums >> 32);
     gaps += (int)all, late += (int)(all >> 32);
+    if (tid == 0) before[words] = gaps;  // (the last time: all of them)
   }
   __syncthreads();
-  // ---- the map: a wave per word of slots; the m-th kept slot from n on goes to the m-th gap
-  for (int w = wave; w < words; w += kChooseWaves) {
-    const uint64_t kept = above[w];
-    const int t = w * 64 + lane;
-    if (!(kept >> lane & 1)) continue;
-    if (t < n) {
-      src[t] = t;
-      continue;
+  // ---- the map: the m-th gap is given the m-th kept slot from n on.  Gaps are listed by rank, as many as the list holds at a time (all
+  // of them up to 16384 slots); a wave takes a word of slots
+  const int n_gaps = before[words];
+  for (int r0 = 0; r0 == 0 || r0 < n_gaps; r0 += p.list) {
+    __syncthreads();
+    for (int w = wave; w <= (n - 1) >> 6; w += kChooseWaves) {
+      const uint64_t kept = above[w];
+      const int t = w * 64 + lane;
+      if (t >= n) continue;
+      if (kept >> lane & 1) {
+        if (r0 == 0) src[t] = t;
+      } else {
+        const int at = before[w] + ones(~kept & ((1ull << lane) - 1)) - r0;
+        if (at >= 0 && at < p.list) list[at] = t;
+      }
     }
-    const int low = n - w * 64;
-    const uint64_t here = low > 0 ? kept & (~0ull << low) : kept;
-    const int rank = rank0[w] + ones(here & ((1ull << lane) - 1));
-    int lo = 0, hi = (n - 1) >> 6;  // the word that holds the gap: the last one with before <= rank
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (before[mid] <= rank) lo = mid;
-      else hi = mid - 1;
+    __syncthreads();
+    for (int w = (n >> 6) + wave; w < words; w += kChooseWaves) {
+      const uint64_t kept = above[w];
+      const int t = w * 64 + lane, low = n - w * 64;
+      const uint64_t late = low > 0 ? kept & (~0ull << low) : kept;
+      const int at = rank0[w] + ones(late & ((1ull << lane) - 1)) - r0;
+      if ((late >> lane & 1) && at >= 0 && at < p.list) src[list[at]] = t;
     }
-    const int room = n - lo * 64;
-    const uint64_t gap = ~above[lo] & (room >= 64 ? ~0ull : (1ull << room) - 1);
-    src[lo * 64 + select_bit(gap, rank - before[lo])] = t;
   }
 }
 
@@ -496,7 +501,8 @@ int tva_evict_select(const tva_evict_select_args *a, void *stream) {
   p.L = a->L, p.keep = a->keep, p.newest = a->newest, p.pos = a->pos, p.weight = a->weight, p.src = a->src, p.L_out = a->L_out;
   p.ld = a->ld, p.ld_src = a->ld_src, p.B = a->B, p.H = a->H, p.max_L = a->max_L, p.n_first = a->n_first;
   p.words = (a->max_L + 63) / 64;
-  const size_t bytes = (size_t)p.words * 24 + kChooseWaves * 8 + (256 * kCopies + 32) * 4;
+  p.list = std::min(a->max_L / 2 + 1, 8192);  // (there are no more gaps than kept slots behind them)
+  const size_t bytes = (size_t)p.words * 24 + 4 + kChooseWaves * 8 + (256 * kCopies + 32 + p.list) * 4;
   const dim3 grid(a->H, a->B, layers), block(kChooseThreads);
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
