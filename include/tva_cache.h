@@ -35,7 +35,7 @@ typedef enum {
  * The first element of KV head g of a position is element page*stride_page + slot*stride_tok + g*stride_head, strides
  * counted in ELEMENTS whatever the kind (page = 0, slot = row in the dense form).  0 = the packed default, [.., Hkv, D]
  * token-major.  BF16: multiples of 8, E4M3: of 16, E2M1: of D (a row's scales are found by element / D).
- * Positions are below 2^30; E2M1 row numbers (element / D) below 2^32.
+ * Positions are below 2^30; E2M1 row numbers (element / D) below 2^32, and stride_tok below 2^25 (2^24 bytes).
  * Head-major ([.., Hkv, page_size, D]: stride_tok = D, stride_head = page_size*D) keeps a head's keys together.
  */
 typedef struct tva_cache {
@@ -91,8 +91,10 @@ size_t tva_sizeof_rows_args(void);
  * tva_tree_verify_attn (tva.h) over a cache of 4-bit rows: sequence b's T_b = cu_T[b+1]-cu_T[b] tree tokens (one: plain
  * decoding) against its L[b] cached tokens and, in bf16, the tree's own K/V under the ancestor sets.  Same shapes,
  * same definition with K and V the values of the rows; out is bf16, rounded once from the fp32 result (the next product
- * takes bf16), lse may be NULL.  A row that attends to nothing gets out = 0, lse = -inf.  num_splits: KV splits per
- * sequence, 0 = the library chooses.  The workspace holds the splits' partial results (0 bytes when there is one split).
+ * takes bf16), lse may be NULL.  A row that attends to nothing gets out = 0, lse = -inf; a tree token's K or V that is not
+ * finite reaches the rows that see it, and no others.  num_splits: into how many parts the keys of each sequence are
+ * split, 0 = the library chooses, and may deal several sequences' keys out together.  The workspace holds partial results
+ * (0 bytes when nothing is split); what it holds before does not matter, and calls that overlap need one each.
  */
 typedef struct tva_attn4_args {
   int32_t B, Hq, Hkv, D;
@@ -118,7 +120,7 @@ typedef struct tva_attn4_args {
 
 int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream);
 size_t tva_attn4_workspace_bytes(const tva_attn4_args *a); /* reads shapes only; (size_t)-1 on invalid ones */
-int32_t tva_attn4_plan_splits(const tva_attn4_args *a);    /* >= 1; -1 on invalid shapes */
+int32_t tva_attn4_plan_splits(const tva_attn4_args *a);    /* parts per sequence, or per 64 sequences dealt out together; -1 on invalid shapes */
 size_t tva_sizeof_attn4_args(void);
 
 /*

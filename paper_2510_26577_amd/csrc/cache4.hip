@@ -9,7 +9,8 @@
 //                      operand's own lanes' (a lane's key, half of the elements) and are widened there; V's pass
 //                      through 4 KB of LDS that belong to the wave, because the transposing read (16 x 16 codes per 16
 //                      lanes) wants rows.  No barrier in the loop.
-//   join_kernel        merges the KV splits' partial results.
+//   join_kernel        merges the partial results of sequences that several workgroups share.
+// Work is dealt out on the device (struct Deal): equal runs of tiles, whatever the sequences' lengths.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -201,10 +202,50 @@ struct FourParams {
   CacheView c;
   __bf16 *out;
   float *lse;
-  float *part_out, *part_lse;  // [S, sum_T * Hq, D], [S, sum_T * Hq] when S > 1
-  int Hq, Hkv, G, W, sum_T, max_L, S, chunk;  // chunk: keys per split, a multiple of 64
-  int tree_split;                             // the split of its own that the tree's keys have, or -1: the last one with cached keys has them
+  float *part_out, *part_lse;  // [slots, Hkv, rows, D], [slots, Hkv, rows]
+  int B, Hq, Hkv, G, W, max_L;
+  int group, parts, rows;  // sequences whose tiles are dealt out together (1, or up to 64), among how many; rows of a slot
   float scale_log2;
+};
+
+// How the tiles of a group of sequences (64 cached keys each, and 64 of the tree's own) are dealt out: in order, in `parts` runs that
+// differ by one tile at most, for one head and block of query rows.  A run may end inside a sequence and go on in the next: lengths
+// that differ cost no balance, and the host need not know them.  A sequence that lies in one run is finished there; of others
+// each run leaves a partial result (in slot run + sequence, which no two share) for join_kernel, which deals out the same way.
+// A sequence by itself (group 1) has its tree's keys in a run of their own: such runs are short, and a tree's tile lasts as long as
+// three of the cache.
+struct Deal {
+  int upto, tiles, t0, T, L;  // this lane's sequence: tiles of the group up to its end, its own; its first node, nodes, cached keys
+  int total, parts;           // tiles and runs of the group
+  int even, even_parts;       // tiles that are dealt out evenly, and among how many runs (the rest is the last run)
+  __device__ __forceinline__ Deal(const FourParams &p, int first, int row0) {
+    tiles = t0 = T = L = 0;
+    if (p.group == 1) {
+      t0 = p.cu_T[first], T = min(p.cu_T[first + 1] - t0, TVA_MAX_TREE), L = min(max(p.L[first], 0), p.max_L);
+      const int cached = (L + 63) >> 6;
+      if (T * p.G > row0) tiles = cached + ((T + 63) >> 6);
+      upto = total = tiles;
+      even = p.parts > 1 ? cached : total, even_parts = min(p.parts > 1 ? p.parts - 1 : 1, even);
+      parts = total == 0 ? 0 : even_parts + (even < total);
+    } else {
+      const int lane = threadIdx.x & 63, b = first + lane;
+      if (lane < p.group && b < p.B) {
+        t0 = p.cu_T[b], T = min(p.cu_T[b + 1] - t0, TVA_MAX_TREE), L = min(max(p.L[b], 0), p.max_L);
+        if (T * p.G > row0) tiles = ((L + 63) >> 6) + ((T + 63) >> 6);
+      }
+      upto = tiles;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        const int y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+      }
+      even = total = __builtin_amdgcn_readlane(upto, 63), even_parts = parts = min(p.parts, total);
+    }
+  }
+  __device__ __forceinline__ static int divide(int64_t x, int y) { return x >> 32 ? (int)(x / y) : (int)((uint32_t)x / (uint32_t)y); }
+  // the first tile of run i (i = parts: the end), and the run that tile x lies in
+  __device__ __forceinline__ int begin(int i) const { return i < even_parts ? divide((int64_t)i * even, even_parts) : i < parts ? even : total; }
+  __device__ __forceinline__ int run_of(int x) const { return x < even ? divide((int64_t)(x + 1) * even_parts + even - 1, even) - 1 : parts - 1; }
 };
 
 __device__ __forceinline__ float half_max(float x) {
@@ -218,29 +259,18 @@ __device__ __forceinline__ float half_sum(float x) {
 
 constexpr int kWaves = 4;
 
-// A node's V may hold what is not finite, and rows that do not see the node must not (0 * inf is NaN): such elements are taken out of
-// the operand, and rows that give them weight get their infinities from products of their own (NaN counts as both).
-__device__ __forceinline__ void add_infinite(bf16x8 &v, const bf16x8 w, f32x16 &acc) {
-  uint16_t x[8];
+// whether any of eight bf16 numbers is infinite or NaN
+__device__ __forceinline__ bool not_finite(u32x4 x) {
   bool any = false;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
-    any |= (x[i] & 0x7f80) == 0x7f80;
-  }
-  if (!__any(any)) return;
-  bf16x8 up, down;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool out = (x[i] & 0x7f80) == 0x7f80, nan = out && (x[i] & 0x7f);
-    up[i] = (__bf16)(out && (nan || x[i] == 0x7f80) ? 1.f : 0.f);
-    down[i] = (__bf16)(out && (nan || x[i] == 0xff80) ? 1.f : 0.f);
-    v[i] = out ? (__bf16)0.f : v[i];
-  }
-  f32x16 zero = {};
-  const f32x16 a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, w, zero, 0, 0, 0), b = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, w, zero, 0, 0, 0);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = (acc[i] + (a[i] > 0.f ? INFINITY : 0.f)) - (b[i] > 0.f ? INFINITY : 0.f);
+  for (int k = 0; k < 4; ++k) any |= (x[k] & 0x7f80) == 0x7f80 || (x[k] & 0x7f800000) == 0x7f800000;
+  return any;
+}
+
+template <bool NT>
+__device__ __forceinline__ u32x4 read_once(const u32x4 *p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
 }
 
 template <int D>
@@ -266,52 +296,121 @@ struct FourCfg {
   static constexpr int LDS = LOOP_LDS > END_LDS ? LOOP_LDS : END_LDS;
 };
 
-// Grid: KV head (fastest: with 8 heads one per XCD), block of WM * 32 query rows, (sequence, split).  The four waves are
-// WM row groups x 4 / WM key groups; tile i of the split belongs to key group i % (4 / WM).
-template <int D, int WM, bool PAGED>
+// Grid: KV head (fastest: with 8 heads one per XCD), block of WM * 32 query rows, run of tiles.  The four waves are WM row groups x
+// 4 / WM key groups; every (4 / WM)th tile of a run's part of a sequence belongs to a key group.
+// PG: 0 dense, 1 paged, 2 paged with pages of whole tiles (one table entry per tile, and as in the dense form addresses that are a
+// scalar and a lane's offset).  NT: one block of rows reads the keys, once.  (64 sequences of 4096 .. 16384 keys, 8 nodes 160 -> 154 us; where
+// blocks share them, 4 sequences of 16384 .. 32768, 48 nodes in two blocks, 147 -> 211.)
+template <int D, int WM, int PG, bool NT>
 __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   typedef FourCfg<D> C;
   constexpr int WK = kWaves / WM;
   __shared__ __align__(16) unsigned char lds[C::LDS];
-  const int g = blockIdx.x, b = blockIdx.z / p.S, split = blockIdx.z - b * p.S;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int g = blockIdx.x, which = blockIdx.z / p.parts, run = blockIdx.z - which * p.parts;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wm = wave % WM, wk = wave / WM;
-  const int t0 = p.cu_T[b], T = min(p.cu_T[b + 1] - t0, TVA_MAX_TREE);
-  const int n_rows = T * p.G;
   const int row0 = blockIdx.y * (WM * 32);
-  if (row0 >= n_rows) return;
-  const int L = min(max(p.L[b], 0), p.max_L);
-  const int last_split = L > 0 ? (L - 1) / p.chunk : 0;
-  const int key0 = split * p.chunk;
-  const int n_keys = split <= last_split && split != p.tree_split ? min(p.chunk, L - key0) : 0;
-  const bool has_tree = split == (p.tree_split < 0 ? last_split : p.tree_split);
-  const int n_cache = (n_keys + 63) >> 6, n_tiles = n_cache + (has_tree ? (T + 63) >> 6 : 0);
+  const Deal deal(p, which * p.group, row0);
+  if (run >= deal.parts) return;
+  int at_tile = deal.begin(run);
+  const int stop = deal.begin(run + 1);
 
-  // this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written
-  const int row = min(row0 + wm * 32 + l32, n_rows - 1);
-  const int node = row / p.G, head = g * p.G + (row - node * p.G);
-  const bool idle = row0 + wm * 32 >= n_rows;
+  while (true) {  // the run's part of one sequence after the other
+    const int lb = __builtin_ctzll(__ballot(deal.upto > at_tile)), b = which * p.group + lb;
+    const int tiles = __builtin_amdgcn_readlane(deal.tiles, lb), seq_end = __builtin_amdgcn_readlane(deal.upto, lb);
+    const int x0 = at_tile - (seq_end - tiles), x1 = min(stop, seq_end) - (seq_end - tiles);  // of the sequence's tiles
+    const bool whole = x1 - x0 == tiles;
+    const int t0 = __builtin_amdgcn_readlane(deal.t0, lb), T = __builtin_amdgcn_readlane(deal.T, lb), L = __builtin_amdgcn_readlane(deal.L, lb);
+    const int n_rows = T * p.G;
+    const int n_cache = (L + 63) >> 6;
 
-  f32x16 acc[C::NJ];
+    // this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written
+    const int row = min(row0 + wm * 32 + l32, n_rows - 1);
+    const int node = row / p.G, head = g * p.G + (row - node * p.G);
+    const bool idle = row0 + wm * 32 >= n_rows;
+
+    unsigned char *vt = lds + wave * C::WAVE_LDS;
+    float *vsl = (float *)(vt + C::VT);
+
+    // ---- what waits in registers: K and V bytes of a tile and their scales ----
+    u32x4 kx[2][C::KL], vx[C::CH];
+    // (scales stay in 16 bits, and what uses them takes the bits it needs: widened, the compiler lets them wait in the loop for what was
+    // only just asked for)
+    uint16_t ks[2], vs;
+    const Finder<PG != 0> find(p.c, b, g);
+    int entry = 0;        // the page of key `lane` of the tile after next (PG 2: of all its keys)
+    uint32_t rs = 0;      // PG 1: the row of key `lane`
+    int64_t base = 0;     // else: the row of the tile's first key
+    const uint32_t step = (uint32_t)p.c.stride_tok;
+    int last = 63;        // rows of the tile past its last key repeat that one and are masked
+    const int cache_end = min(x1, n_cache);
+    auto look = [&](int tile) __attribute__((always_inline)) {
+      tile = min(tile, cache_end - 1);
+      if constexpr (PG == 1) entry = find.entry(p.c, min(tile * 64 + lane, L - 1));
+      if constexpr (PG == 2) entry = find.entry(p.c, tile * 64);
+    };
+    auto place = [&](int tile) __attribute__((always_inline)) {
+      last = min(63, L - 1 - tile * 64);
+      if constexpr (PG == 1) rs = (uint32_t)find.at(p.c, min(tile * 64 + lane, L - 1), entry);  // (row numbers have 32 bits)
+      else base = find.at(p.c, tile * 64, __builtin_amdgcn_readfirstlane(entry));
+    };
+    // key r's row (PG 1), or its distance from the tile's first; and byte `at` of that row in a tensor of `size` bytes per row, where it
+    // can be as a scalar and a lane's 32-bit offset
+    auto row_of = [&](int r) __attribute__((always_inline)) -> uint32_t {
+      if constexpr (PG == 1) return (uint32_t)__shfl((int)rs, r);
+      else return __umul24(min(r, last), step);
+    };
+    auto byte_of = [&](const char *from, uint32_t row, int size, int at) __attribute__((always_inline)) -> const char * {
+      if constexpr (PG == 1) return from + ((uint64_t)row * (uint32_t)size + (uint32_t)at);
+      else return from + base * size + (uint32_t)(row * (uint32_t)size + at);
+    };
+    // What a lane works out from its number is worked out again in every tile: kept, it takes the registers that the loop needs, and
+    // what is then read back from memory waits for all loads on their way.
+    auto afresh = [&](int tile) __attribute__((always_inline)) {
+      int x;
+      asm("" : "=v"(x) : "0"(lane), "s"(tile));
+      return x;
+    };
+    auto fetch_k = [&](int tile) __attribute__((always_inline)) {
+      const int ln = afresh(tile), hf = ln >> 5;
 #pragma unroll
-  for (int j = 0; j < C::NJ; ++j)
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t row = row_of(kb * 32 + (ln & 31));
+        const char *from = byte_of(p.c.k, row, C::RB, hf * (C::RB / 2));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
-  float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
+        for (int i = 0; i < C::KL; ++i) kx[kb][i] = read_once<NT>((const u32x4 *)(from + i * 16));
+        if constexpr (D == 128) ks[kb] = *(const uint16_t *)byte_of(p.c.k_row_scale, row, 4, hf * 2);
+        else ks[kb] = *(const uint8_t *)byte_of(p.c.k_row_scale, row, 2, hf);
+      }
+    };
+    auto fetch_v = [&](int tile) __attribute__((always_inline)) {
+      const int ln = afresh(tile);
+#pragma unroll
+      for (int i = 0; i < C::CH; ++i) vx[i] = read_once<NT>((const u32x4 *)byte_of(p.c.v, row_of(i * C::RPL + ln / C::CH), C::RB, (ln % C::CH) * 16));
+      if constexpr (PG == 1) vs = *(const uint16_t *)(p.c.v_row_scale + (uint64_t)rs * 2);
+      else vs = *(const uint16_t *)byte_of(p.c.v_row_scale, row_of(ln), 2, 0);
+    };
 
-  if (n_tiles > 0) {
+    int tile = x0 + wk;
+    if (!idle && tile < cache_end) look(tile), place(tile), fetch_k(tile), fetch_v(tile), look(tile + WK);
+
+    bf16x8 q[C::NS];
+    const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(qrow + s * 8);
+
     // ancestor set of this lane's node, trimmed to the tree
     uint64_t anc0 = 0, anc1 = 0;
-    if (has_tree) {
+    if (x1 > n_cache) {
       if (p.mask) {
         const uint64_t *w = p.mask + (int64_t)(t0 + node) * p.W;
         anc0 = w[0];
         if (p.W > 1) anc1 = w[1];
       } else {
         int32_t *par = (int32_t *)(lds + kWaves * C::WAVE_LDS);
-        if (tid < T && tid < TVA_MAX_TREE) par[tid] = p.parent[t0 + tid];
+        if (tid < T) par[tid] = p.parent[t0 + tid];
         __syncthreads();
-        int a = min(node, TVA_MAX_TREE - 1);
+        int a = node;
         for (int step = 0; step < TVA_MAX_TREE; ++step) {
           if (a < 64) anc0 |= 1ull << a;
           else anc1 |= 1ull << (a - 64);
@@ -324,57 +423,10 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
       else if (T < 128) anc1 &= (1ull << (T - 64)) - 1;
     }
 
-    unsigned char *vt = lds + wave * C::WAVE_LDS;
-    float *vsl = (float *)(vt + C::VT);
-
-    // ---- what waits in registers: K and V bytes of a tile and their scales ----
-    u32x4 kx[2][C::KL], vx[C::CH];
-    uint32_t ks[2];
-    uint16_t vs;
-    const Finder<PAGED> find(p.c, b, g);
-    // a tile's rows past the end repeat the last one and are masked
-    auto own = [&](int key) __attribute__((always_inline)) { return key0 + min(key, n_keys - 1); };
-    // rows of the tile's keys: K's (this lane's key in each block of 32), V's (the rows its loads cover), and key `lane`; paged: each
-    // lane has the table entry of key `lane`, looked up a tile earlier, and hands its row to the others
-    int entry = 0;
-    auto look = [&](int tile) __attribute__((always_inline)) {
-      if constexpr (PAGED) entry = find.entry(p.c, own(tile * 64 + lane));
-    };
-    auto fetch = [&](int tile) __attribute__((always_inline)) {
-      int64_t rk[2], rv[C::CH];
-      const int64_t rs = find.at(p.c, own(tile * 64 + lane), entry);
-      if constexpr (PAGED) {
-        auto of = [&](int l) __attribute__((always_inline)) { return (int64_t)(uint32_t)__shfl((int)rs, l); };  // (row numbers have 32 bits)
+    f32x16 acc[C::NJ];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) rk[kb] = of(kb * 32 + l32);
-#pragma unroll
-        for (int i = 0; i < C::CH; ++i) rv[i] = of(i * C::RPL + lane / C::CH);
-      } else {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) rk[kb] = find.at(p.c, own(tile * 64 + kb * 32 + l32), 0);
-#pragma unroll
-        for (int i = 0; i < C::CH; ++i) rv[i] = find.at(p.c, own(tile * 64 + i * C::RPL + lane / C::CH), 0);
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int i = 0; i < C::KL; ++i) kx[kb][i] = *(const u32x4 *)(p.c.k + rk[kb] * C::RB + half * (C::RB / 2) + i * 16);
-        if constexpr (D == 128) ks[kb] = *(const uint16_t *)(p.c.k_row_scale + rk[kb] * 4 + half * 2);
-        else ks[kb] = *(const uint8_t *)(p.c.k_row_scale + rk[kb] * 2 + half);
-      }
-#pragma unroll
-      for (int i = 0; i < C::CH; ++i) vx[i] = *(const u32x4 *)(p.c.v + rv[i] * C::RB + (lane % C::CH) * 16);
-      vs = *(const uint16_t *)(p.c.v_row_scale + rs * 2);
-    };
-
-    int tile = wk;
-    if (!idle && tile < n_cache) look(tile), fetch(tile), look(tile + WK);
-    bf16x8 q[C::NS];
-    const __bf16 *qrow = p.q + ((int64_t)(t0 + node) * p.Hq + head) * D + half * (D / 2);
-#pragma unroll
-    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(qrow + s * 8);
-
-
+    for (int j = 0; j < C::NJ; ++j) acc[j] = f32x16{};
+    float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
     f32x16 s[2];
     // scores -> probabilities in place (log2 domain, fp32), O and l moved to a new reference where a row's maximum grew
     auto soften = [&]() __attribute__((always_inline)) {
@@ -405,51 +457,54 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     };
 
     if (!idle) {
-      for (; tile < n_cache; tile += WK) {
+      for (; tile < cache_end; tile += WK) {
+        // ---- S^T = K Q^T
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < C::NS; ++st)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            const float sc = __uint_as_float(((uint32_t)ks[kb] << (st < C::NS / 2 || D == 64 ? 23 : 15)) & 0x7f800000u);  // exponent_byte
+            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(kx[kb][st / 4][st % 4], sc), q[st], s[kb], 0, 0, 0);
+          }
+        const int left = L - tile * 64;
+        // (the next tile, or the last one again: a branch here would leave the waits without a count to go by)
+        place(min(tile + WK, cache_end - 1)), fetch_k(tile), look(tile + 2 * WK);
+        if (left < 64) {
+          const int mine = left - 4 * (afresh(tile) >> 5);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (kb * 32 + 8 * (i / 4) + i % 4 >= mine) s[kb][i] = -INFINITY;
+        }
+        soften();
+        const int ln = afresh(tile);
         // ---- V to LDS: piece c of row r lies at piece c ^ (r / 8) of its row, so that the 16 rows a transposing read takes
         // together (4 consecutive ones of each 8) are in different banks
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < C::CH; ++i) {
-          const int r = i * C::RPL + lane / C::CH;
-          *(u32x4 *)(vt + r * C::RB + (((lane % C::CH) ^ (r >> 3)) & (C::CH - 1)) * 16) = vx[i];
+          const int r = i * C::RPL + ln / C::CH;
+          *(u32x4 *)(vt + r * C::RB + (((ln % C::CH) ^ (r >> 3)) & (C::CH - 1)) * 16) = vx[i];
         }
-        vsl[lane] = __uint_as_float((uint32_t)vs << 16);
+        vsl[ln] = __uint_as_float((uint32_t)vs << 16);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        // ---- S^T = K Q^T
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-#pragma unroll
-        for (int st = 0; st < C::NS; ++st)
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            const float sc = exponent_byte(st < C::NS / 2 || D == 64 ? ks[kb] & 255 : ks[kb] >> 8);
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(kx[kb][st / 4][st % 4], sc), q[st], s[kb], 0, 0, 0);
-          }
-        const int left = n_keys - tile * 64;
-        if (tile + WK < n_cache) fetch(tile + WK), look(tile + 2 * WK);
-        if (left < 64) {
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (kb * 32 + 8 * (i / 4) + 4 * half + i % 4 >= left) s[kb][i] = -INFINITY;
-        }
-        soften();
-        // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight
+        fetch_v(tile);
+        // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight (rounded to bf16 with it: the
+        // operand's type; half a step, 2^-8, of a weight)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           bf16x8 w[2];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const f32x4 sc = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * half);
+            const f32x4 sc = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * (ln >> 5));
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[i / 2][(i % 2) * 4 + k] = (__bf16)(s[kb][i * 4 + k] * sc[k]);
           }
           // this lane's row of the 16 x 16 codes its 16 lanes turn over: key slot i of its half, 8 bytes of elements
-          const int i16 = lane & 15, r = kb * 32 + 8 * (i16 >> 2) + 4 * half + (i16 & 3), sub = (lane >> 4) & 1;
+          const int i16 = ln & 15, r = kb * 32 + 8 * (i16 >> 2) + 4 * (ln >> 5) + (i16 & 3), sub = (ln >> 4) & 1;
 #pragma unroll
           for (int j = 0; j < C::NJ; ++j) {
             const i32x2 c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
@@ -460,8 +515,9 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         }
       }
       // ---- the tree's own keys, bf16: V goes to LDS while K's rows are fetched and multiplied
-      for (; tile < n_tiles; tile += WK) {
+      for (; tile < x1; tile += WK) {
         const int first = (tile - n_cache) * 64, left = T - first;
+        const int lane = afresh(tile), l32 = lane & 31, half = lane >> 5;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int n = 0; n < C::NB; ++n) {
@@ -490,6 +546,34 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         soften();
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): V is in LDS
         asm volatile("" ::: "memory");
+        // A node's V may hold what is not finite, and rows that do not see the node must not (0 * inf is NaN): such elements are taken
+        // out of the tile, and rows that see them get them added
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < C::NB; ++n) odd |= not_finite(*(const u32x4 *)(vt + n * C::BLK + lane * 16));
+        if (__any(odd)) {
+          for (int n = 0; n < C::NB; ++n) {
+            u32x4 x = *(const u32x4 *)(vt + n * C::BLK + lane * 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if ((x[k] & 0x7f80) == 0x7f80) x[k] &= 0xffff0000u;
+              if ((x[k] & 0x7f800000) == 0x7f800000) x[k] &= 0xffffu;
+            }
+            *(u32x4 *)(vt + n * C::BLK + lane * 16) = x;
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          for (int k = 0; k < min(left, 64); ++k) {
+            const bool sees = ((first ? anc1 : anc0) >> k) & 1;
+            const __bf16 *vrow = p.v_tree + ((int64_t)(t0 + first + k) * p.Hkv + g) * D + 4 * half;
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float v = (float)vrow[32 * j + 8 * (i / 4) + i % 4];
+                if (sees && !__builtin_isfinite(v)) acc[j][i] += v;
+              }
+          }
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -509,78 +593,87 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
                 c[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (__attribute__((address_space(3))) s16x4 *)(vt + (r % C::NB) * C::BLK + (r / C::NB) * (D * 2) + j * 64 + sub * 32 + (i16 & 3) * 8));
               }
-              bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
-              add_infinite(v, w, acc[j]);
+              const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
               acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
             }
           }
       }
     }
-  }
 
-  // ---- the key groups' results joined, and O^T turned over to rows ----
-  l = half_sum(l);
-  __syncthreads();
-  float *patch = (float *)lds, *maxima = (float *)(lds + kWaves * C::PATCH), *sums = maxima + kWaves * 32;
-  if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
-  __syncthreads();
-  float top = -INFINITY;
+    // ---- the key groups' results joined, and O^T turned over to rows ----
+    l = half_sum(l);
+    __syncthreads();
+    float *patch = (float *)lds, *maxima = (float *)(lds + kWaves * C::PATCH), *sums = maxima + kWaves * 32;
+    if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
+    __syncthreads();
+    float top = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < WK; ++k) top = fmaxf(top, maxima[(k * WM + wm) * 32 + l32]);
-  float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    for (int k = 0; k < WK; ++k) top = fmaxf(top, maxima[(k * WM + wm) * 32 + l32]);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
-  for (int j = 0; j < C::NJ; ++j)
+    for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f32x4 x;
+      for (int i = 0; i < 4; ++i) {
+        f32x4 x;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = acc[j][i * 4 + k] * f;
-      *(f32x4 *)(patch + wave * (32 * C::TP) + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
+        for (int k = 0; k < 4; ++k) x[k] = acc[j][i * 4 + k] * f;
+        *(f32x4 *)(patch + wave * (32 * C::TP) + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
+      }
+    __syncthreads();
+    constexpr int PIECES = WM * 32 * (D / 4);
+    const int64_t slot = ((int64_t)(which * (p.parts + p.group) + run + lb) * p.Hkv + g) * p.rows;
+    for (int x = tid; x < PIECES; x += 256) {
+      const int r = x / (D / 4), d = (x - r * (D / 4)) * 4, w = r >> 5, rr = r & 31;
+      if (row0 + r >= n_rows) break;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      float top_r = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < WK; ++k) top_r = fmaxf(top_r, maxima[(k * WM + w) * 32 + rr]);
+#pragma unroll
+      for (int k = 0; k < WK; ++k) {
+        const int at = k * WM + w;
+        o += *(const f32x4 *)(patch + at * (32 * C::TP) + rr * C::TP + d);
+        const float mk = maxima[at * 32 + rr];
+        sum += mk == -INFINITY ? sums[at * 32 + rr] : sums[at * 32 + rr] * __builtin_amdgcn_exp2f(mk - top_r);  // (0, or NaN)
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
+      o *= inv;
+      const float lse = sum == 0.f ? -INFINITY : (top_r + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
+      if (whole) {
+        const int rnode = (row0 + r) / p.G, rhead = g * p.G + (row0 + r - rnode * p.G);
+        const int64_t at = (int64_t)(t0 + rnode) * p.Hq + rhead;
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = (__bf16)o[k];
+        *(bf16x4 *)(p.out + at * D + d) = y;
+        if (d == 0 && p.lse) p.lse[at] = lse;
+      } else {
+        *(f32x4 *)(p.part_out + (slot + row0 + r) * D + d) = o;
+        if (d == 0) p.part_lse[slot + row0 + r] = lse;
+      }
     }
-  __syncthreads();
-  constexpr int PIECES = WM * 32 * (D / 4);
-  for (int x = tid; x < PIECES; x += 256) {
-    const int r = x / (D / 4), d = (x - r * (D / 4)) * 4, w = r >> 5, rr = r & 31;
-    if (row0 + r >= n_rows) break;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float top_r = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < WK; ++k) top_r = fmaxf(top_r, maxima[(k * WM + w) * 32 + rr]);
-#pragma unroll
-    for (int k = 0; k < WK; ++k) {
-      const int at = k * WM + w;
-      o += *(const f32x4 *)(patch + at * (32 * C::TP) + rr * C::TP + d);
-      const float mk = maxima[at * 32 + rr];
-      sum += mk == -INFINITY ? sums[at * 32 + rr] : sums[at * 32 + rr] * __builtin_amdgcn_exp2f(mk - top_r);  // (0, or NaN)
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
-    o *= inv;
-    const int rnode = (row0 + r) / p.G, rhead = g * p.G + (row0 + r - rnode * p.G);
-    const int64_t at = (int64_t)(t0 + rnode) * p.Hq + rhead;
-    const float lse = sum == 0.f ? -INFINITY : (top_r + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
-    if (p.S > 1) {
-      const int64_t n = (int64_t)p.sum_T * p.Hq;
-      if (sum != 0.f) *(f32x4 *)(p.part_out + ((int64_t)split * n + at) * D + d) = o;
-      if (d == 0) p.part_lse[(int64_t)split * n + at] = lse;
-    } else {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 y;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = (__bf16)o[k];
-      *(bf16x4 *)(p.out + at * D + d) = y;
-      if (d == 0 && p.lse) p.lse[at] = lse;
-    }
+    at_tile = seq_end;
+    if (at_tile >= stop) return;
+    __syncthreads();  // (the patches are read before the next sequence's tiles take their place)
   }
 }
 
-// Splits of one row per D/4 lanes: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s.  Eight splits are in flight at a
-// time; what a split without keys holds is read and dropped.
+// The parts of sequences that several runs share, merged: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s, D/4 lanes per
+// row.  Grid: KV head, 1024 / D query rows, sequence (block_rows: the attention's).  Eight parts are in flight at a time.
 template <int D>
-__global__ void __launch_bounds__(256) join_kernel(const float *part_out, const float *part_lse, int S, int64_t n, __bf16 *out, float *lse) {
-  constexpr int LPR = D / 4, U = 8;
-  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+__global__ void __launch_bounds__(256) join_kernel(const FourParams p, int block_rows) {
+  constexpr int LPR = D / 4, U = 8, ROWS = 256 / LPR;
+  const int g = blockIdx.x, row = blockIdx.y * ROWS + threadIdx.x / LPR, row0 = blockIdx.y * ROWS / block_rows * block_rows, b = blockIdx.z, which = b / p.group, lb = b - which * p.group;
+  const Deal deal(p, which * p.group, row0);
+  const int tiles = __builtin_amdgcn_readlane(deal.tiles, lb), end = __builtin_amdgcn_readlane(deal.upto, lb);
+  if (tiles == 0) return;
+  const int first = deal.run_of(end - tiles), S = deal.run_of(end - 1) - first + 1;
+  if (S == 1) return;
+  const int t0 = __builtin_amdgcn_readlane(deal.t0, lb), n_rows = __builtin_amdgcn_readlane(deal.T, lb) * p.G;
+  const int64_t stride = (int64_t)p.Hkv * p.rows, slot0 = (int64_t)(which * (p.parts + p.group) + first + lb) * stride + (int64_t)g * p.rows;
   const int d = (threadIdx.x % LPR) * 4;
-  if (row >= n) return;
+  if (row >= n_rows) return;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float top = -INFINITY, sum = 0.f;
   for (int s0 = 0; s0 < S; s0 += U) {
@@ -588,9 +681,9 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part_out, const 
     f32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = (int64_t)min(s0 + u, S - 1) * n + row;
-      ls[u] = part_lse[at];
-      x[u] = *(const f32x4 *)(part_out + at * D + d);
+      const int64_t at = slot0 + min(s0 + u, S - 1) * stride + row;
+      ls[u] = p.part_lse[at];
+      x[u] = *(const f32x4 *)(p.part_out + at * D + d);
     }
     float here = top;
 #pragma unroll
@@ -599,7 +692,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part_out, const 
     o *= f, sum *= f, top = here;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (s0 + u >= S || ls[u] == -INFINITY) continue;  // (nothing was written there)
+      if (s0 + u >= S || ls[u] == -INFINITY) continue;
       const float w = __builtin_amdgcn_exp2f((ls[u] - (top == -INFINITY ? 0.f : top)) * kLog2e);
       sum += w;
       o += x[u] * w;
@@ -610,35 +703,40 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part_out, const 
   bf16x4 y;
 #pragma unroll
   for (int k = 0; k < 4; ++k) y[k] = (__bf16)(o[k] * inv);
-  *(bf16x4 *)(out + row * D + d) = y;
-  if (d == 0 && lse) lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+  const int node = row / p.G, head = g * p.G + (row - node * p.G);
+  const int64_t at = (int64_t)(t0 + node) * p.Hq + head;
+  *(bf16x4 *)(p.out + at * D + d) = y;
+  if (d == 0 && p.lse) p.lse[at] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
 struct FourPlan {
-  int WM, blocks, S, chunk;
-  bool tree_alone;
+  int WM, blocks, group, groups, parts;
 };
+// 32-row workgroups while there is little work: their four waves split the keys, which costs no partial results (one sequence of 2048
+// keys, 60 nodes: 14.8 us with 32 rows, 19.4 with 64, 25.5 with 128).  Else as many rows as divide the row groups without waste, so
+// that fewer workgroups read the same keys (4 sequences of 16384 .. 32768, 48 nodes, six groups: 64 rows 119 us, 128 rows 147).
+// Long work of several sequences is dealt out over two workgroups per CU; a sequence by itself over one (the case above with 256
+// workgroups 14.8 us, with 512 18.5), and one run at most is a round short of a workgroup rather than one too many.
 void plan_four(const tva_attn4_args *a, FourPlan *pl) {
+  constexpr int kSlots = 256, kTogether = 6;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G, groups = std::max<int64_t>(1, (rows + 31) / 32);
-  const int tiles = std::max(1, (a->max_L + 63) / 64);
+  const int tiles = (a->max_L + 63) / 64 + (a->max_T + 63) / 64;
   const int64_t pairs = (int64_t)a->B * a->Hkv;
   if (a->plan_rows) pl->WM = a->plan_rows / 32;
   else pl->WM = pairs * groups * tiles <= 4 * 2048 || groups == 1 ? 1 : groups % 4 == 0 || groups > 8 ? 4 : groups % 2 == 0 ? 2 : groups == 3 ? 4 : 1;
-  pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
-  const int64_t base = pairs * pl->blocks;
   const int WK = kWaves / pl->WM;
-  int64_t S = a->num_splits;
-  if (S == 0) {
-    S = (512 + base - 1) / base;                                      // two workgroups per CU
-    S = std::min<int64_t>(S, std::max(1, (tiles + WK - 1) / WK));  // a tile per wave
+  pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
+  const int64_t base = (int64_t)a->Hkv * pl->blocks;
+  const int64_t load = pairs * pl->blocks * tiles / (2 * kSlots * WK);  // tiles a wave has where two workgroups per CU share them
+  pl->group = a->B > 1 && load >= kTogether && a->num_splits == 0 ? (int)std::min(a->B, 64) : 1;
+  pl->groups = (a->B + pl->group - 1) / pl->group;
+  int64_t parts = a->num_splits;
+  if (parts == 0) {
+    parts = std::max<int64_t>(1, (pl->group > 1 ? 2 * kSlots : kSlots) / (base * pl->groups));
+    if (pl->group == 1) parts = std::min<int64_t>(parts, std::max(1, (tiles + WK - 1) / WK));  // a tile per wave
   }
-  S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
-  const int per = (int)((tiles + S - 1) / S);
-  pl->chunk = per * 64;
-  pl->S = (tiles + per - 1) / per;
-  pl->tree_alone = pl->S > 1;
-  pl->S += pl->tree_alone;
+  pl->parts = (int)std::max<int64_t>(1, std::min<int64_t>(parts, (int64_t)pl->group * tiles));
 }
 
 int check_four(const tva_attn4_args *a, bool shapes_only) {
@@ -659,7 +757,8 @@ int check_four(const tva_attn4_args *a, bool shapes_only) {
 }
 
 size_t four_bytes(const tva_attn4_args *a, const FourPlan &pl) {
-  return pl.S <= 1 ? 0 : (size_t)pl.S * a->sum_T * a->Hq * (a->D + 1) * 4;
+  const size_t slots = (size_t)pl.groups * (pl.parts + pl.group), rows = (size_t)pl.blocks * pl.WM * 32;
+  return pl.parts == 1 ? 0 : slots * a->Hkv * rows * (a->D + 1) * 4;
 }
 
 template <int D>
@@ -714,7 +813,7 @@ int32_t tva_attn4_plan_splits(const tva_attn4_args *a) {
   FourPlan pl;
   if (check_four(a, true) != TVA_OK) return -1;
   plan_four(a, &pl);
-  return pl.S;
+  return pl.parts;
 }
 
 int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream) {
@@ -729,24 +828,35 @@ int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream) {
   const size_t need = four_bytes(a, pl);
   if (need && (!a->workspace || ((uintptr_t)a->workspace & 15))) return TVA_INVALID_ARG;
   if (a->workspace_bytes < need) return TVA_WORKSPACE_TOO_SMALL;
-  if ((int64_t)a->B * pl.S > 65535 || pl.blocks > 65535) return TVA_UNSUPPORTED;
+  if ((int64_t)pl.groups * pl.parts > 65535 || a->B > 65535 || pl.blocks > 65535) return TVA_UNSUPPORTED;
+  if (p.c.stride_tok * (a->D / 2) >= 1 << 24) return TVA_UNSUPPORTED;  // (offsets within a tile)
   p.q = (const __bf16 *)a->q, p.k_tree = (const __bf16 *)a->k_tree, p.v_tree = (const __bf16 *)a->v_tree;
   p.cu_T = a->cu_T, p.L = a->L, p.parent = a->parent, p.mask = a->anc_mask;
   p.out = (__bf16 *)a->out, p.lse = a->lse;
-  const int64_t n = (int64_t)a->sum_T * a->Hq;
-  p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (pl.S > 1 ? pl.S * n * a->D : 0);
-  p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.sum_T = a->sum_T, p.max_L = a->max_L;
-  p.S = pl.S, p.chunk = pl.chunk, p.tree_split = pl.tree_alone ? pl.S - 1 : -1, p.scale_log2 = a->scale * kLog2e;
-  const dim3 grid(a->Hkv, pl.blocks, a->B * pl.S);
+  p.rows = pl.blocks * pl.WM * 32;
+  p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (need ? need / 4 / (a->D + 1) * a->D : 0);
+  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.max_L = a->max_L;
+  p.group = pl.group, p.parts = pl.parts, p.scale_log2 = a->scale * kLog2e;
+  const dim3 grid(a->Hkv, pl.blocks, pl.groups * pl.parts);
   const hipStream_t st = (hipStream_t)stream;
-  const bool paged = a->cache.page_table != nullptr;
+  const int pg = !a->cache.page_table ? 0 : a->cache.page_size % 64 ? 1 : 2;
   (void)hipGetLastError();
   auto launch = [&](auto d, auto wm) {
     constexpr int D = decltype(d)::value, WM = decltype(wm)::value;
-    if (paged) hipLaunchKernelGGL((four_bit_kernel<D, WM, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((four_bit_kernel<D, WM, false>), grid, dim3(256), 0, st, p);
-    if (pl.S > 1 && hipPeekAtLastError() == hipSuccess)
-      hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)((n + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, p.part_out, p.part_lse, pl.S, n, p.out, p.lse);
+    auto form = [&](auto nt) {
+      constexpr bool NT = decltype(nt)::value;
+      if (pg == 0) hipLaunchKernelGGL((four_bit_kernel<D, WM, 0, NT>), grid, dim3(256), 0, st, p);
+      else if (pg == 1) hipLaunchKernelGGL((four_bit_kernel<D, WM, 1, NT>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((four_bit_kernel<D, WM, 2, NT>), grid, dim3(256), 0, st, p);
+    };
+    if constexpr (WM == 1) {
+      if (pl.blocks == 1) form(std::true_type{});
+      else form(std::false_type{});
+    } else {
+      form(std::false_type{});
+    }
+    if (pl.parts > 1 && hipPeekAtLastError() == hipSuccess)
+      hipLaunchKernelGGL(join_kernel<D>, dim3(a->Hkv, (p.rows + 1024 / D - 1) / (1024 / D), a->B), dim3(256), 0, st, p, WM * 32);
   };
   auto shapes = [&](auto d) {
     if (pl.WM == 1) launch(d, std::integral_constant<int, 1>{});
