@@ -193,7 +193,7 @@ struct ChooseParams {
   int B, H, max_L, n_first, words, list;  // words: 64-slot words of the longest row; list: gaps listed at a time
 };
 
-constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kCopies = 16;
+constexpr int kChooseThreads = 512, kChooseWaves = kChooseThreads / 64, kCopies = 16;
 
 // Slots in the order they are kept: larger first.  Protected above everything, NaN below, -0 as 0.
 __device__ __forceinline__ uint32_t key_of(const ChooseParams &p, float w, bool safe) {
@@ -237,9 +237,9 @@ __device__ __forceinline__ T scan_threads(T x, T *part, T *total) {
   return x + before;
 }
 
-// ITEMS > 0: the row's keys stay in registers (L <= 1024 * ITEMS); 0: they are read again in every pass.
+// ITEMS > 0: the row's keys stay in registers (L <= kChooseThreads * ITEMS); 0: they are read again in every pass.
 template <int ITEMS>
-__global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseParams p) {
+__global__ void __launch_bounds__(kChooseThreads, 4) choose_kernel(const ChooseParams p) {
   extern __shared__ __align__(16) unsigned char lds[];
   uint64_t *above = (uint64_t *)lds, *equal = above + p.words;  // a bit per slot; above becomes the kept set
   uint64_t *part64 = equal + p.words;                            // kChooseWaves
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChoosePara
   // Slots from L on count as the smallest key there is: they come last among equals, behind all that n < L can reach.
   // Reads are batched, ROUNDS of the workgroup at a time (one by one each waits for the one before: 512 rows of up to 32768 slots with
   // ages 164 us instead of 114).
-  constexpr int ROUNDS = ITEMS > 0 && ITEMS < 8 ? ITEMS : 8;
+  constexpr int ROUNDS = 4;
   auto read = [&](int t0, uint32_t (&k)[ROUNDS]) __attribute__((always_inline)) {
     float w[ROUNDS];
     int age[ROUNDS];
@@ -506,9 +506,9 @@ int tva_evict_select(const tva_evict_select_args *a, void *stream) {
   const dim3 grid(a->H, a->B, layers), block(kChooseThreads);
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
-  if (a->max_L <= 4 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<4>, grid, block, bytes, st, p);
-  else if (a->max_L <= 16 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<16>, grid, block, bytes, st, p);
+  if (a->max_L <= 8 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<8>, grid, block, bytes, st, p);
   else if (a->max_L <= 32 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<32>, grid, block, bytes, st, p);
+  else if (a->max_L <= 64 * kChooseThreads) hipLaunchKernelGGL(choose_kernel<64>, grid, block, bytes, st, p);
   else hipLaunchKernelGGL(choose_kernel<0>, grid, block, bytes, st, p);
   return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
 }

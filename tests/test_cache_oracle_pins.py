@@ -178,6 +178,11 @@ def test_attention_refuses_other_caches_and_takes_nothing_for_nothing(lib):
     assert lib.tva_tree_verify_attn_4bit(ctypes.byref(_attn(sum_T=0)), None) == 0 and lib.tva_tree_verify_attn_4bit(ctypes.byref(_attn(max_T=0)), None) == 0
 
 
+def test_attention_refuses_strides_whose_tiles_need_longer_offsets(lib):
+    for D, most in ((128, 1 << 25), (64, 1 << 25)):
+        assert lib.tva_tree_verify_attn_4bit(ctypes.byref(_attn(_cache(stride_tok=most), D=D, num_splits=1)), None) == -2
+
+
 def test_attention_plan(lib):
     for B in (1, 3, 64):
         for L in (0, 1, 64, 65, 1000, 32768):

@@ -123,7 +123,7 @@ def test_rows_without_a_place_are_left_out(torch, page):
 
 # ---- attention ----
 def _attend(torch, rng, heads, sizes, lengths, page=0, head_major=False, splits=0, by_parent=False, scale=None, spread=1.0, mask=None, k_tree=None,
-            v_tree=None, q=None, max_L=None, check=True):
+            v_tree=None, q=None, max_L=None, check=True, rows=0):
     from paper_2510_26577_amd import cache4
     Hq, Hkv, D = heads
     B, n = len(sizes), sum(sizes)
@@ -144,7 +144,7 @@ def _attend(torch, rng, heads, sizes, lengths, page=0, head_major=False, splits=
     kw = dict(parent=cc.dev(np.concatenate(parents))) if by_parent else dict(anc_mask=cc.dev(sets))
     args = cache4.make_attn_args(q=cc.dev(q), k_tree=cc.dev(k_tree), v_tree=cc.dev(v_tree), cache=cache.cache, cu_T=cc.dev(cu),
                                  L=cc.dev(np.array(lengths, np.int32)), max_T=max(sizes), max_L=max(lengths) if max_L is None else max_L,
-                                 scale=scale, out=out, lse=lse, num_splits=splits, **kw)
+                                 scale=scale, out=out, lse=lse, num_splits=splits, plan_rows=rows, **kw)
     ws = cache4.attn_workspace(args, "cuda")
     if ws is not None:
         ws.fill_(float("nan"))
@@ -204,6 +204,28 @@ def test_attention_over_trees(torch, T, by_parent):
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_in_splits(torch, splits, D):
     _attend(torch, np.random.default_rng(splits), (8, 2, D), [9, 40, 3, 1], [1000, 130, 0, 64], 16, splits=splits)
+
+
+@pytest.mark.parametrize("rows", [32, 64, 128])
+@pytest.mark.parametrize("D,page", [(64, 0), (128, 0), (128, 16), (64, 64), (128, 64)])
+def test_attention_with_rows_named(torch, rows, D, page):
+    """Every size of a workgroup, with trees that fill part of one, one, and several."""
+    rng = np.random.default_rng(rows)
+    for splits in (0, 3):
+        _attend(torch, rng, (12, 2, D), [70, 1, 6, 22], [333, 40, 64, 200], page, splits=splits, rows=rows)
+
+
+@pytest.mark.parametrize("D,page,head_major", [(64, 0, True), (128, 64, False), (64, 16, False)])
+def test_attention_of_many_sequences_dealt_out_together(torch, D, page, head_major):
+    """More sequences than are dealt out together (64), of lengths that differ, some without a tree, some without a context."""
+    from paper_2510_26577_amd import cache4
+    rng = np.random.default_rng(D)
+    lengths = rng.integers(0, 2000, 70).tolist()
+    lengths[3], lengths[40], lengths[66] = 0, 1999, 64
+    sizes = rng.integers(1, 4, 70).tolist()
+    sizes[5] = sizes[63] = 0
+    args, *_ = _attend(torch, rng, (8, 8, D), sizes, lengths, page, head_major)
+    assert cache4.plan_splits(args) > 20  # (a sequence alone would have one)
 
 
 def test_attention_of_empty_trees_and_masks_without_keys(torch):
