@@ -57,10 +57,24 @@ def _lib():
     return lib
 
 
+def _whole(**tensors) -> None:
+    """What is passed as an address and sizes alone is packed."""
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name} is not contiguous")
+
+
+def _indices(**tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and (t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous()):
+            raise ValueError(f"{name} is a contiguous int32 tensor")
+
+
 def make_cache(*, k, v=None, k_row_scale=None, v_row_scale=None, kind: int = ROWS_E2M1, cu_L=None, page_table=None, page_size: int = 0,
                strides=(0, 0, 0), k_scale: float = 1.0, v_scale: float = 1.0) -> Cache:
     """A cache's tensors, any shape: where a row lies is said by the strides (elements of page, token, head; 0 = packed
     token-major).  v may be left out where only K is read (evict.key_weights)."""
+    _indices(cu_L=cu_L, page_table=page_table)
     c = Cache()
     c.kind, c.page_size, c.max_pages = int(kind), int(page_size), int(page_table.shape[1]) if page_table is not None else 0
     c.k_scale, c.v_scale = float(k_scale), float(v_scale)
@@ -76,6 +90,8 @@ def make_cache(*, k, v=None, k_row_scale=None, v_row_scale=None, kind: int = ROW
 def make_rows_args(*, k_rows, v_rows, cu_T, L, cache: Cache, max_rows: int, path=None, path_len=None, L_out=None, err_flag=None,
                    n_layers: int = 0, layer_stride_cache: int = 0, layer_stride_rows: int = 0) -> RowsArgs:
     """k_rows, v_rows: bf16 [.., Hkv, D] (with n_layers > 1 the first layer's lead, the others layer_stride_rows elements further on)."""
+    _whole(k_rows=k_rows, v_rows=v_rows)
+    _indices(cu_T=cu_T, L=L, path=path, path_len=path_len, L_out=L_out, err_flag=err_flag)
     a = RowsArgs()
     a.B, a.Hkv, a.D, a.max_rows = cu_T.numel() - 1, int(k_rows.shape[-2]), int(k_rows.shape[-1]), int(max_rows)
     if path is not None and int(path.shape[1]) != a.max_rows:
@@ -110,6 +126,8 @@ def load(*, stream=None, **kw) -> None:
 def make_attn_args(*, q, k_tree, v_tree, cache: Cache, cu_T, L, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
                    lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0) -> Attn4Args:
     """q bf16 [sum_T, Hq, D], k_tree / v_tree bf16 [sum_T, Hkv, D], out bf16 like q, lse fp32 [sum_T, Hq] or None."""
+    _whole(q=q, k_tree=k_tree, v_tree=v_tree, anc_mask=anc_mask, out=out, lse=lse, workspace=workspace)
+    _indices(cu_T=cu_T, L=L, parent=parent)
     a = Attn4Args()
     a.B = cu_T.numel() - 1
     a.sum_T, a.Hq, a.D = (int(s) for s in q.shape)

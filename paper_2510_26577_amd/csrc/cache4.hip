@@ -729,7 +729,8 @@ void plan_four(const tva_attn4_args *a, FourPlan *pl) {
   pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
   const int64_t base = (int64_t)a->Hkv * pl->blocks;
   const int64_t load = pairs * pl->blocks * tiles / (2 * kSlots * WK);  // tiles a wave has where two workgroups per CU share them
-  pl->group = a->B > 1 && load >= kTogether && a->num_splits == 0 ? (int)std::min(a->B, 64) : 1;
+  pl->groups = a->B > 1 && load >= kTogether && a->num_splits == 0 ? (a->B + 63) / 64 : a->B;
+  pl->group = (a->B + pl->groups - 1) / pl->groups;
   pl->groups = (a->B + pl->group - 1) / pl->group;
   int64_t parts = a->num_splits;
   if (parts == 0) {
@@ -763,7 +764,7 @@ size_t four_bytes(const tva_attn4_args *a, const FourPlan &pl) {
 
 template <int D>
 int launch_rows(const RowsParams &p, int B, int layers, bool load, hipStream_t st) {
-  const int64_t groups = ((int64_t)p.max_rows * p.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8));
+  const int64_t groups = std::max<int64_t>(1, ((int64_t)p.max_rows * p.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8)));  // (one writes L_out)
   if (groups > 0x7fffffff) return TVA_UNSUPPORTED;
   const dim3 grid((unsigned)groups, B, (layers + kRowLayers - 1) / kRowLayers);
   if (load) hipLaunchKernelGGL(load_rows_kernel<D>, grid, dim3(256), 0, st, p);
@@ -785,7 +786,7 @@ int run_rows(const tva_rows_args *a, bool load, void *stream) {
   RowsParams p{};
   const int rc = view_of(a->cache, a->Hkv, a->D, true, &p.c);
   if (rc != TVA_OK) return rc;
-  if (a->max_rows == 0) return TVA_OK;
+  if (a->max_rows == 0 && !a->L_out) return TVA_OK;
   p.cu_T = a->cu_T, p.L = a->L, p.path = a->path, p.path_len = a->path_len;
   p.k_rows = (uint16_t *)a->k_rows, p.v_rows = (uint16_t *)a->v_rows;
   p.L_out = a->L_out, p.err_flag = a->err_flag, p.Hkv = a->Hkv, p.max_rows = a->max_rows, p.n_layers = layers;

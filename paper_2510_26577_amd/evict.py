@@ -7,7 +7,7 @@ import ctypes
 
 from . import binding
 from .binding import _p
-from .cache4 import Cache
+from .cache4 import Cache, _indices, _whole
 
 _ready = False
 
@@ -52,6 +52,8 @@ def _lib():
 def make_key_weight_args(*, q, lse, cache: Cache, cu_T, L, weight, max_rows: int, max_L: int, scale: float, path=None, path_len=None,
                          pos=None, first_pos=None) -> KeyWeightArgs:
     """q bf16 [sum_T, Hq, D] and lse fp32 [sum_T, Hq] of a step's attention; weight fp32 (and pos int32) [B, Hkv, ld]."""
+    _whole(q=q, lse=lse, weight=weight)
+    _indices(cu_T=cu_T, L=L, path=path, path_len=path_len, pos=pos, first_pos=first_pos)
     a = KeyWeightArgs()
     a.B, a.Hq, a.Hkv, a.D = cu_T.numel() - 1, int(q.shape[1]), int(weight.shape[1]), int(q.shape[2])
     a.max_rows, a.max_L, a.scale = int(max_rows), int(max_L), float(scale)
@@ -68,6 +70,8 @@ def make_key_weight_args(*, q, lse, cache: Cache, cu_T, L, weight, max_rows: int
 
 def make_select_args(*, weight, L, keep, max_L: int, src, L_out=None, n_first: int = 0, newest=None, pos=None) -> SelectArgs:
     """weight fp32 (and pos int32) [n_layers, B, H, ld] or [B, H, ld], src int32 likewise with ld_src."""
+    _whole(weight=weight)
+    _indices(L=L, keep=keep, src=src, L_out=L_out, newest=newest, pos=pos)
     a = SelectArgs()
     if tuple(src.shape[:-1]) != tuple(weight.shape[:-1]) or (pos is not None and tuple(pos.shape) != tuple(weight.shape)):
         raise ValueError("weight, pos and src have the same rows")
@@ -82,6 +86,8 @@ def make_select_args(*, weight, L, keep, max_L: int, src, L_out=None, n_first: i
 def make_move_args(*, src, n, cache: Cache, Hkv: int, D: int, max_keep: int, weight=None, pos=None, layer_stride_cache: int = 0,
                    err_flag=None) -> MoveArgs:
     """src int32 [n_layers, B, H, ld_src] or [B, H, ld_src] (H = Hkv, or 1: shared by the heads), n: select's L_out."""
+    _whole(weight=weight)
+    _indices(src=src, n=n, pos=pos, err_flag=err_flag)
     a = MoveArgs()
     for t in (weight, pos):
         if t is not None and tuple(t.shape[:-1]) != tuple(src.shape[:-1]):

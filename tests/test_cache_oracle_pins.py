@@ -136,7 +136,7 @@ def test_store_and_load_refuse_what_is_no_call(lib):
     assert lib.tva_cache_load(ctypes.byref(_rows(L_out=8192)), None) == -1
     for kind in (cache4.ROWS_BF16, cache4.ROWS_E4M3):
         assert lib.tva_cache_store(ctypes.byref(_rows(_cache(kind=kind))), None) == -2
-    assert lib.tva_cache_store(ctypes.byref(_rows(B=0)), None) == 0 and lib.tva_cache_store(ctypes.byref(_rows(max_rows=0)), None) == 0
+    assert lib.tva_cache_store(ctypes.byref(_rows(B=0)), None) == 0 and lib.tva_cache_store(ctypes.byref(_rows(max_rows=0, L_out=None)), None) == 0
 
 
 @pytest.mark.parametrize("kw,code", BAD_CACHES)
@@ -261,6 +261,8 @@ def test_move_refuses(lib, kw, code):
 def test_python_calls_refuse_shapes_that_do_not_fit(lib):
     import torch
     c = cache4.make_cache(k=torch.zeros(64, dtype=torch.uint8), cu_L=torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        cache4.make_cache(k=torch.zeros(64, dtype=torch.uint8), cu_L=torch.zeros(2))
     rows, ints = torch.zeros((4, 2, 64), dtype=torch.bfloat16), torch.zeros((1, 4), dtype=torch.int32)
     with pytest.raises(ValueError):
         cache4.make_rows_args(k_rows=rows, v_rows=rows, cu_T=ints[0, :2], L=ints[0], cache=c, max_rows=3, path=ints, path_len=ints[0])
@@ -273,3 +275,8 @@ def test_python_calls_refuse_shapes_that_do_not_fit(lib):
         evict.make_move_args(src=torch.zeros((1, 2, 8), dtype=torch.int32), n=ints, cache=c, Hkv=2, D=64, max_keep=8, weight=torch.zeros((1, 1, 8)))
     with pytest.raises(TypeError):
         cache4.store_raw(evict.SelectArgs())
+    n = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="not contiguous"):
+        evict.make_select_args(weight=torch.zeros((1, 2, 16))[..., :8], L=n, keep=n, max_L=8, src=torch.zeros((1, 2, 8), dtype=torch.int32))
+    with pytest.raises(ValueError, match="int32"):
+        evict.make_select_args(weight=w, L=n.long(), keep=n, max_L=8, src=torch.zeros((1, 2, 8), dtype=torch.int32))

@@ -121,6 +121,16 @@ def test_rows_without_a_place_are_left_out(torch, page):
         assert set(changed.tolist()) == own
 
 
+def test_lengths_are_written_without_rows_too(torch):
+    from paper_2510_26577_amd import cache4
+    rng = np.random.default_rng(15)
+    lay = cc.Layout(rng, [8, 8], 2, 128)
+    cache = cc.FourBit(rng, lay, [3, 5])
+    L_out, rows = torch.full((2,), -1, dtype=torch.int32, device="cuda"), cc.dev(_rows(rng, (2, 2, 128)))
+    cache4.store(k_rows=rows, v_rows=rows, cu_T=cc.dev([0, 1, 2], np.int32), L=cc.dev([3, 5], np.int32), cache=cache.cache, max_rows=0, L_out=L_out)
+    assert L_out.tolist() == [3, 5] and np.array_equal(cache.download()[0], cache.k)
+
+
 # ---- attention ----
 def _attend(torch, rng, heads, sizes, lengths, page=0, head_major=False, splits=0, by_parent=False, scale=None, spread=1.0, mask=None, k_tree=None,
             v_tree=None, q=None, max_L=None, check=True, rows=0):
