@@ -494,24 +494,34 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         fetch_v(tile);
         // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight (rounded to bf16 with it: the
         // operand's type; half a step, 2^-8, of a weight)
+        // (all operands are read ahead: each where it is used, 4 sequences of 16384 .. 32768 keys, 48 nodes, take 124 us instead of 117)
+        i32x2 c[2][C::NJ];
+        f32x4 sc[2][4];
+        {
+          // this lane's row of the 16 x 16 codes its 16 lanes turn over: key slot i of its half, 8 bytes of elements
+          const int i16 = ln & 15, sub = (ln >> 4) & 1;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            const int r = kb * 32 + 8 * (i16 >> 2) + 4 * (ln >> 5) + (i16 & 3);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[kb][i] = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * (ln >> 5));
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j)
+              c[kb][j] = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                  (__attribute__((address_space(3))) i32x2 *)(vt + r * C::RB + ((j ^ (r >> 3)) & (C::CH - 1)) * 16 + sub * 8));
+          }
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           bf16x8 w[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 sc = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * (ln >> 5));
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[i / 2][(i % 2) * 4 + k] = (__bf16)(s[kb][i * 4 + k] * sc[k]);
-          }
-          // this lane's row of the 16 x 16 codes its 16 lanes turn over: key slot i of its half, 8 bytes of elements
-          const int i16 = ln & 15, r = kb * 32 + 8 * (i16 >> 2) + 4 * (ln >> 5) + (i16 & 3), sub = (ln >> 4) & 1;
+            for (int k = 0; k < 4; ++k) w[i / 2][(i % 2) * 4 + k] = (__bf16)(s[kb][i * 4 + k] * sc[kb][i][k]);
 #pragma unroll
-          for (int j = 0; j < C::NJ; ++j) {
-            const i32x2 c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-                (__attribute__((address_space(3))) i32x2 *)(vt + r * C::RB + ((j ^ (r >> 3)) & (C::CH - 1)) * 16 + sub * 8));
+          for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
-            for (int a = 0; a < 2; ++a) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)c[a], 1.f), w[a], acc[j], 0, 0, 0);
-          }
+            for (int a = 0; a < 2; ++a) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)c[kb][j][a], 1.f), w[a], acc[j], 0, 0, 0);
         }
       }
       // ---- the tree's own keys, bf16: V goes to LDS while K's rows are fetched and multiplied
