@@ -267,6 +267,68 @@ def test_entries_that_are_no_moves_are_left_out(torch):
 
 
 # ---- together ----
+def test_a_step_in_a_graph_and_on_another_stream(torch):
+    """Commit, weights, choice and move captured once: every replay gives what the eager calls give, on a stream of their own too."""
+    from paper_2510_26577_amd import cache4, evict
+    rng = np.random.default_rng(31)
+    Hq, Hkv, D, layers, T, L0 = 8, 2, 128, 2, 10, [60, 150]
+    lay = cc.Layout(rng, [160, 160], Hkv, D, 16)
+    four = cc.FourBit(rng, lay, L0, layers)
+    k, v = (cc.dev(orc.to_bf16(rng.standard_normal((layers, 2 * T, Hkv, D)))) for _ in range(2))
+    q, lse = cc.dev(orc.to_bf16(rng.standard_normal((2 * T, Hq, D)))), cc.dev(np.full((2 * T, Hq), 5.0, np.float32))
+    cu_T, L, keep = cc.dev([0, T, 2 * T], np.int32), cc.dev(L0, np.int32), cc.dev([50, 100], np.int32)
+    path, n = cc.dev([[0, 3, 7], [0, 1, -1]], np.int32), cc.dev([3, 2], np.int32)
+    weight, pos = cc.dev(rng.random((layers, 2, Hkv, 160)).astype(np.float32)), torch.zeros((layers, 2, Hkv, 160), dtype=torch.int32, device="cuda")
+    L_new, L_kept, flag = (torch.zeros(m, dtype=torch.int32, device="cuda") for m in (2, 2, 1))
+    src = torch.zeros((layers, 2, Hkv, 100), dtype=torch.int32, device="cuda")
+    store = cache4.make_rows_args(k_rows=k, v_rows=v, cu_T=cu_T, L=L, cache=four.cache, max_rows=3, path=path, path_len=n, L_out=L_new, err_flag=flag,
+                                  n_layers=layers, layer_stride_cache=lay.rows * D, layer_stride_rows=2 * T * Hkv * D)
+    weigh = [evict.make_key_weight_args(q=q, lse=lse, cache=lay.cache(**{x: t[i * lay.rows:(i + 1) * lay.rows] for x, t in four.d.items()}), cu_T=cu_T,
+                                        L=L_new, weight=weight[i], pos=pos[i], first_pos=L, max_rows=3, max_L=160, scale=0.1, path=path, path_len=n)
+             for i in range(layers)]
+    choose = evict.make_select_args(weight=weight, L=L_new, keep=keep, max_L=160, src=src, L_out=L_kept, n_first=2, newest=L, pos=pos)
+    shift = evict.make_move_args(src=src, n=L_kept, cache=four.cache, Hkv=Hkv, D=D, max_keep=100, weight=weight, pos=pos,
+                                 layer_stride_cache=lay.rows * D, err_flag=flag)
+    state = [*four.d.values(), weight, pos, src, L_new, L_kept]
+    first = [t.clone() for t in state]
+
+    def reset():
+        for t, x in zip(state, first):
+            t.copy_(x)
+
+    def step(stream=None):
+        cache4.store_raw(store, stream)
+        for a in weigh:
+            evict.key_weights_raw(a, stream)
+        evict.select_raw(choose, stream)
+        evict.move_raw(shift, stream)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in state]
+    assert L_kept.tolist() == [50, 100] and not flag.item() and not torch.equal(want[0], first[0])
+    same = lambda: all(torch.equal(t.view(torch.uint8), x.view(torch.uint8)) for t, x in zip(state, want))
+    other = torch.cuda.Stream()
+    reset()
+    torch.cuda.synchronize()
+    step(other)
+    other.synchronize()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        step()
+    for _ in range(4):
+        reset()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same()
+        reset()
+        step()
+        torch.cuda.synchronize()
+        assert same()
+
+
 def test_a_cache_over_its_budget(torch):
     """Prompts stored, then steps of attention, acceptance, commit and weighing; whenever a sequence is over the budget its slots are
     chosen and moved.  Every step's attention is compared with 64 bits on the values the cache should hold."""
