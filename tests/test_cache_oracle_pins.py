@@ -280,3 +280,17 @@ def test_python_calls_refuse_shapes_that_do_not_fit(lib):
         evict.make_select_args(weight=torch.zeros((1, 2, 16))[..., :8], L=n, keep=n, max_L=8, src=torch.zeros((1, 2, 8), dtype=torch.int32))
     with pytest.raises(ValueError, match="int32"):
         evict.make_select_args(weight=w, L=n.long(), keep=n, max_L=8, src=torch.zeros((1, 2, 8), dtype=torch.int32))
+
+
+def test_kernels_of_long_caches_keep_their_registers(lib):
+    """No vector register goes to memory, and as many wavefronts fit as the kernels' workgroups per compute unit need."""
+    from tests.test_kernel_resources import kernels
+    most = {"four_bit_kernel": 256, "join_kernel": 128, "weigh_kernel": 170, "choose_kernel": 128, "shift_kernel": 64, "store_rows_kernel": 128,
+            "load_rows_kernel": 64}
+    seen = dict.fromkeys(most, 0)
+    for name, k in kernels().items():
+        for part, limit in most.items():
+            if part in name:
+                seen[part] += 1
+                assert k[".vgpr_spill_count"] == 0 and k[".vgpr_count"] <= limit, (name, k[".vgpr_count"], k[".vgpr_spill_count"])
+    assert all(seen.values()), seen
