@@ -722,24 +722,25 @@ __global__ void __launch_bounds__(256) join_kernel(const FourParams p, int block
 struct FourPlan {
   int WM, blocks, group, groups, parts;
 };
-// 32-row workgroups while there is little work: their four waves split the keys, which costs no partial results (one sequence of 2048
-// keys, 60 nodes: 14.8 us with 32 rows, 19.4 with 64, 25.5 with 128).  Else as many rows as divide the row groups without waste, so
+// 32-row workgroups while there is little work and one round of them holds it: their four waves split the keys, which costs no partial
+// results (one sequence of 2048 keys, 60 nodes: 14.8 us with 32 rows, 19.4 with 64, 25.5 with 128; but 26 sequences of 7 keys, 64
+// heads, 64 nodes 72 us with 32 rows, 42 with 128).  Else as many rows as divide the row groups without waste, so
 // that fewer workgroups read the same keys (4 sequences of 16384 .. 32768, 48 nodes, six groups: 64 rows 119 us, 128 rows 147).
-// Long work of several sequences is dealt out over two workgroups per CU; a sequence by itself over one (the case above with 256
+// Long work of several long sequences is dealt out over two workgroups per CU (a part of a sequence costs about four tiles of its own); a sequence by itself over one (the case above with 256
 // workgroups 14.8 us, with 512 18.5), and one run at most is a round short of a workgroup rather than one too many.
 void plan_four(const tva_attn4_args *a, FourPlan *pl) {
-  constexpr int kSlots = 256, kTogether = 6;
+  constexpr int kSlots = 256, kTogether = 6, kLong = 32;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G, groups = std::max<int64_t>(1, (rows + 31) / 32);
   const int tiles = (a->max_L + 63) / 64 + (a->max_T + 63) / 64;
   const int64_t pairs = (int64_t)a->B * a->Hkv;
   if (a->plan_rows) pl->WM = a->plan_rows / 32;
-  else pl->WM = pairs * groups * tiles <= 4 * 2048 || groups == 1 ? 1 : groups % 4 == 0 || groups > 8 ? 4 : groups % 2 == 0 ? 2 : groups == 3 ? 4 : 1;
+  else pl->WM = groups == 1 || (pairs * groups <= 2 * kSlots && pairs * groups * tiles <= 8 * 2048) ? 1 : groups % 4 == 0 || groups > 8 ? 4 : groups % 2 == 0 ? 2 : groups == 3 ? 4 : 1;
   const int WK = kWaves / pl->WM;
   pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
   const int64_t base = (int64_t)a->Hkv * pl->blocks;
   const int64_t load = pairs * pl->blocks * tiles / (2 * kSlots * WK);  // tiles a wave has where two workgroups per CU share them
-  pl->groups = a->B > 1 && load >= kTogether && a->num_splits == 0 ? (a->B + 63) / 64 : a->B;
+  pl->groups = a->B > 1 && load >= kTogether && tiles >= kLong && a->num_splits == 0 ? (a->B + 63) / 64 : a->B;
   pl->group = (a->B + pl->groups - 1) / pl->groups;
   pl->groups = (a->B + pl->group - 1) / pl->group;
   int64_t parts = a->num_splits;
