@@ -91,10 +91,12 @@ size_t tva_sizeof_rows_args(void);
  * tva_tree_verify_attn (tva.h) over a cache of 4-bit rows: sequence b's T_b = cu_T[b+1]-cu_T[b] tree tokens (one: plain
  * decoding) against its L[b] cached tokens and, in bf16, the tree's own K/V under the ancestor sets.  Same shapes,
  * same definition with K and V the values of the rows; out is bf16, rounded once from the fp32 result (the next product
- * takes bf16), lse may be NULL.  A row that attends to nothing gets out = 0, lse = -inf; a tree token's K or V that is not
- * finite reaches the rows that see it, and no others.  num_splits: into how many parts the keys of each sequence are
- * split, 0 = the library chooses, and may deal several sequences' keys out together.  The workspace holds partial results
- * (0 bytes when nothing is split); what it holds before does not matter, and calls that overlap need one each.
+ * takes bf16), lse may be NULL.  Sums and softmax weights are fp32; as a factor of V a weight has 16 bits, that of a cached key
+ * with no more than an eighth of its row possibly 8 (half a step, 2^-8 of that weight, as in tva_tree_verify_attn).
+ * A row that attends to nothing gets out = 0, lse = -inf; a tree token's K or V that is not finite reaches the rows that see
+ * it, and no others.  num_splits: into how many parts the keys of each sequence are split, 0 = the library chooses, and may
+ * deal several sequences' keys out together.  The workspace holds partial results (0 bytes when nothing is split); what it
+ * holds before does not matter, and calls that overlap need one each.
  */
 typedef struct tva_attn4_args {
   int32_t B, Hq, Hkv, D;
@@ -104,7 +106,7 @@ typedef struct tva_attn4_args {
   float scale;
   int32_t num_splits;
   int32_t plan_rows;           /* query rows (nodes x heads of a KV head) per workgroup: 32, 64 or 128; 0 = the library chooses.  A
-                                  tuning and testing aid: every value computes the same for every input, in another order */
+                                  tuning and testing aid: every value computes the same for every input, to the roundings above */
   int32_t reserved;
   const int32_t *cu_T, *L;     /* device [B+1], [B] */
   const void *q;               /* device bf16 [sum_T, Hq, D] */

@@ -259,6 +259,21 @@ __device__ __forceinline__ float half_sum(float x) {
 
 constexpr int kWaves = 4;
 
+// A weight is rounded to bf16, the operand's type: half a step, 2^-8 of it.  Where many keys share a row the roundings cancel below that of
+// the result; where few do they show.  So what the rounding leaves is multiplied too (2^-17 of a weight is then off) wherever a row's
+// largest weight in a tile is more than this share of what the row has summed: no weight beyond an eighth of its row goes without.
+constexpr float kLoThreshold = 0.125f;
+// What is left of two numbers when their bf16 roundings (h) are taken from them, as bf16.  One instruction each, two where the
+// rounding is widened first.  Its second operands, (-1, 0) and (0, -1), are in registers: as inline constants they are not read as bf16.
+struct Remainders {
+  uint32_t first = 0xbf80u, second = 0xbf800000u;
+  __device__ __forceinline__ Remainders() { asm("" : "+s"(first), "+s"(second)); }
+  __device__ __forceinline__ bf16x2 of(float x, float y, bf16x2 h) const {
+    return bf16x2{(__bf16)__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, first), x, false),
+                  (__bf16)__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, second), y, false)};
+  }
+};
+
 // whether any of eight bf16 numbers is infinite or NaN
 __device__ __forceinline__ bool not_finite(u32x4 x) {
   bool any = false;
@@ -305,6 +320,11 @@ template <int D, int WM, int PG, bool NT>
 __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   typedef FourCfg<D> C;
   constexpr int WK = kWaves / WM;
+  // Remainders in every tile, or in a block of their own where some row needs them.  In every tile where several 32-row blocks share the
+  // keys, which mostly is work of a few tiles per wave that need them all (one sequence of 2048 keys, 60 nodes: 15.4 us, 16.6 with the
+  // block, 14.5 without remainders); else few tiles need them (64 sequences of 4096 .. 16384 keys, 8 nodes: 182 us, 165, 160; 4 of
+  // 16384 .. 32768, 48 nodes: 141 us, 124, 117).
+  constexpr bool ALWAYS = WM == 1 && !NT;
   __shared__ __align__(16) unsigned char lds[C::LDS];
   const int g = blockIdx.x, which = blockIdx.z / p.parts, run = blockIdx.z - which * p.parts;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -428,8 +448,9 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     for (int j = 0; j < C::NJ; ++j) acc[j] = f32x16{};
     float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
     f32x16 s[2];
-    // scores -> probabilities in place (log2 domain, fp32), O and l moved to a new reference where a row's maximum grew
-    auto soften = [&]() __attribute__((always_inline)) {
+    // scores -> probabilities in place (log2 domain, fp32), O and l moved to a new reference where a row's maximum grew.  Returns whether
+    // a row's largest one is beyond kLoThreshold.
+    auto soften = [&]() __attribute__((always_inline)) -> bool {
       float top = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -454,7 +475,9 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
           s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, -ref));
           l += s[kb][i];
         }
+      return __any(__builtin_amdgcn_exp2f(top - ref) > kLoThreshold * half_sum(l));
     };
+    const Remainders remainders;
 
     if (!idle) {
       for (; tile < cache_end; tile += WK) {
@@ -479,7 +502,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
             for (int i = 0; i < 16; ++i)
               if (kb * 32 + 8 * (i / 4) + i % 4 >= mine) s[kb][i] = -INFINITY;
         }
-        soften();
+        const bool fine = soften();
         const int ln = afresh(tile);
         // ---- V to LDS: piece c of row r lies at piece c ^ (r / 8) of its row, so that the 16 rows a transposing read takes
         // together (4 consecutive ones of each 8) are in different banks
@@ -492,8 +515,37 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         vsl[ln] = __uint_as_float((uint32_t)vs << 16);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         fetch_v(tile);
-        // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight (rounded to bf16 with it: the
-        // operand's type; half a step, 2^-8, of a weight)
+        // ---- O^T += V^T (P s_v)^T; codes are widened as they are, their row's scale is in the weight and rounded to bf16 with it
+        // Remainders in a block of their own, which reads its operands for itself: kept for it, they would take registers in every tile.
+        // (With ALWAYS: below.)
+        if (!ALWAYS && fine) {
+          int ln;
+          asm volatile("" : "=v"(ln) : "0"(lane) : "memory");
+          const int i16 = ln & 15, sub = (ln >> 4) & 1;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            const int r = kb * 32 + 8 * (i16 >> 2) + 4 * (ln >> 5) + (i16 & 3);
+            bf16x8 w[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f32x4 sc = *(const f32x4 *)(vsl + kb * 32 + 8 * i + 4 * (ln >> 5));
+#pragma unroll
+              for (int k = 0; k < 4; k += 2) {
+                const float x = s[kb][i * 4 + k] * sc[k], y = s[kb][i * 4 + k + 1] * sc[k + 1];
+                const bf16x2 rest = remainders.of(x, y, bf16x2{(__bf16)x, (__bf16)y});
+                w[i / 2][(i % 2) * 4 + k] = rest[0], w[i / 2][(i % 2) * 4 + k + 1] = rest[1];
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j) {
+              const i32x2 x = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                  (__attribute__((address_space(3))) i32x2 *)(vt + r * C::RB + ((j ^ (r >> 3)) & (C::CH - 1)) * 16 + sub * 8));
+#pragma unroll
+              for (int a = 0; a < 2; ++a) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)x[a], 1.f), w[a], acc[j], 0, 0, 0);
+            }
+          }
+        }
+        if constexpr (!ALWAYS) asm volatile("" ::: "memory");
         // (all operands are read ahead: each where it is used, 4 sequences of 16384 .. 32768 keys, 48 nodes, take 124 us instead of 117)
         i32x2 c[2][C::NJ];
         f32x4 sc[2][4];
@@ -513,15 +565,27 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          bf16x8 w[2];
+          bf16x8 w[2], low[2];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[i / 2][(i % 2) * 4 + k] = (__bf16)(s[kb][i * 4 + k] * sc[kb][i][k]);
+            for (int k = 0; k < 4; k += 2) {
+              const float x = s[kb][i * 4 + k] * sc[kb][i][k], y = s[kb][i * 4 + k + 1] * sc[kb][i][k + 1];
+              const bf16x2 h = {(__bf16)x, (__bf16)y};
+              w[i / 2][(i % 2) * 4 + k] = h[0], w[i / 2][(i % 2) * 4 + k + 1] = h[1];
+              if constexpr (ALWAYS) {
+                const bf16x2 rest = remainders.of(x, y, h);
+                low[i / 2][(i % 2) * 4 + k] = rest[0], low[i / 2][(i % 2) * 4 + k + 1] = rest[1];
+              }
+            }
 #pragma unroll
           for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
-            for (int a = 0; a < 2; ++a) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)c[kb][j][a], 1.f), w[a], acc[j], 0, 0, 0);
+            for (int a = 0; a < 2; ++a) {
+              const bf16x8 v = widen8((uint32_t)c[kb][j][a], 1.f);
+              acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[a], acc[j], 0, 0, 0);
+              if constexpr (ALWAYS) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low[a], acc[j], 0, 0, 0);
+            }
         }
       }
       // ---- the tree's own keys, bf16: V goes to LDS while K's rows are fetched and multiplied
@@ -553,7 +617,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
           for (int i = 0; i < 16; ++i)
             if (!((bits >> (8 * (i / 4) + 4 * half + i % 4)) & 1)) s[kb][i] = -INFINITY;
         }
-        soften();
+        (void)soften();
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): V is in LDS
         asm volatile("" ::: "memory");
         // A node's V may hold what is not finite, and rows that do not see the node must not (0 * inf is NaN): such elements are taken
@@ -589,9 +653,12 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
             if (kb * 32 + a * 16 >= left) continue;
-            bf16x8 w;
+            bf16x8 w, low;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[kb][a * 8 + i];
+            for (int i = 0; i < 8; i += 2) {
+              const bf16x2 h = {(__bf16)s[kb][a * 8 + i], (__bf16)s[kb][a * 8 + i + 1]}, rest = remainders.of(s[kb][a * 8 + i], s[kb][a * 8 + i + 1], h);
+              w[i] = h[0], w[i + 1] = h[1], low[i] = rest[0], low[i + 1] = rest[1];
+            }
             // 16 lanes turn over 4 rows x 16 elements: this lane's row (of keys 8 c + 4 half + 0..3) and 8-byte piece of it
             const int i16 = lane & 15, sub = (lane >> 4) & 1;
 #pragma unroll
@@ -605,6 +672,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
               }
               const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
               acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
+              acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low, acc[j], 0, 0, 0);  // (a tree's keys are few: in any case)
             }
           }
       }
