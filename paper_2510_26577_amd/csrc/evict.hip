@@ -121,17 +121,24 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
     const int r = min(r0 + l32, R - 1), i = r / p.G, head = g * p.G + (r - i * p.G);
     const int node = p.path ? p.path[(int64_t)b * p.max_rows + i] : i;
     const bool there = node >= 0 && node < T;
-    const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
-    const float lse = p.lse[row];
-    const bool counts = there && r0 + l32 < R && lse != -INFINITY;
-    const __bf16 *from = p.q + row * D;
+    bool counts = false;
+    float minus = 0.f;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      q[s] = *(const bf16x8 *)(from + (KIND == TVA_ROWS_BF16 ? s * 16 + half * 8 : half * (D / 2) + s * 8));
-      if (!counts) q[s] = bf16x8{};  // (whatever it holds)
+    for (int s = 0; s < NS; ++s) q[s] = bf16x8{};
+    if (T > 0) {  // (a sequence without rows has none to read, and the last one's would lie behind the tensors)
+      const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
+      const float lse = p.lse[row];
+      counts = there && r0 + l32 < R && lse != -INFINITY;
+      const __bf16 *from = p.q + row * D;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        q[s] = *(const bf16x8 *)(from + (KIND == TVA_ROWS_BF16 ? s * 16 + half * 8 : half * (D / 2) + s * 8));
+        if (!counts) q[s] = bf16x8{};  // (whatever it holds)
+      }
+      minus = -lse * kLog2e;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (half == 0) to[0][l32] = counts ? -lse * kLog2e : -INFINITY, to[1][l32] = __int_as_float(old + i);
+    if (half == 0) to[0][l32] = counts ? minus : -INFINITY, to[1][l32] = __int_as_float(old + i);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   // a block's products with a block of rows, as weights, added to this lane's key's sum (of this half's rows)

@@ -1,0 +1,48 @@
+"""Key weights (include/tva_cache.h) where rows are missing or keys are not finite."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as orc
+from tests import cache_cases as cc
+from tests.test_gpu_evict import torch  # noqa: F401  (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _close(got, ref, off, rows):
+    """The bounds of test_gpu_evict.test_key_weights: 2^-20 of the exponentials' arguments, sums of `rows` terms in fp32."""
+    tol = 2.0 ** -20 * off + 2.0 ** -22 * (rows + 2) * np.abs(ref) + 1e-30
+    assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) / tol).max()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e2m1"])
+@pytest.mark.parametrize("sizes", [[5, 0], [0, 5, 0], [0, 4, 0, 0]])
+def test_a_path_through_no_tree_adds_nothing(torch, sizes, kind):
+    """Sequences without rows whose path has entries all the same: none is a row, the last sequence's would lie behind q and lse."""
+    from paper_2510_26577_amd import cache4, evict
+    rng = np.random.default_rng(len(sizes))
+    Hq, Hkv, D, L, n = 8, 2, 128, 70, 3
+    B, rows = len(sizes), sum(sizes)
+    lay = cc.Layout(rng, [L] * B, Hkv, D, 16)
+    if kind == "e2m1":
+        four = cc.FourBit(rng, lay, [L] * B)
+        cache, K = four.cache, [four.values(b, np.arange(L))[0] for b in range(B)]
+    else:
+        x = orc.to_bf16(rng.standard_normal((lay.rows, D)))
+        cache, K = lay.cache(kind=cache4.ROWS_BF16, k=cc.dev(x)), [orc.bf16(x[lay.at(b, np.arange(L))]) for b in range(B)]
+    q = orc.to_bf16(rng.standard_normal((rows, Hq, D)))
+    lse = (rng.random((rows, Hq)) * 3 + 3).astype(np.float32)
+    w0 = rng.random((B, Hkv, L)).astype(np.float32)
+    w, pos = cc.dev(w0), torch.full((B, Hkv, L), -3, dtype=torch.int32, device="cuda")
+    cu = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    path = np.tile(np.arange(n, dtype=np.int32), (B, 1))
+    evict.key_weights(q=cc.dev(q), lse=cc.dev(lse), cache=cache, cu_T=cc.dev(cu), L=cc.dev([L] * B, np.int32), weight=w, max_rows=n, max_L=L, scale=0.1,
+                      path=cc.dev(path), path_len=cc.dev([n] * B, np.int32), pos=pos, first_pos=cc.dev(np.arange(B) * 100, np.int32))
+    torch.cuda.synchronize()
+    got = w.cpu().numpy()
+    for b in range(B):
+        at = cu[b] + np.arange(n)
+        l = lse[at].astype(np.float64) if sizes[b] else np.full((n, Hq), -np.inf)
+        ref, off = orc.key_weights(w0[b], orc.bf16(q[at]) if sizes[b] else np.zeros((n, Hq, D)), l, K[b], n, 0.1)
+        _close(got[b], ref, off, n * Hq // Hkv)
+        assert (pos[b, :, L - n:].cpu().numpy() == b * 100 + np.arange(n)).all() and (pos[b, :, :L - n] == -3).all()
