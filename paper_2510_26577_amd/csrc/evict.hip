@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
   for (int u = 0; u < AHEAD; ++u) entry[u] = find.entry(p.c, own(key0 + 32 * (AHEAD + u)));
 
   const int R = n * p.G;
-  // rows r0 .. r0+31: query operand (a row per lane), and in LDS minus log-sum-exp and the last position the row saw
+  // rows r0 .. r0+31: query operand (a row per lane), and in LDS minus log-sum-exp and the last position the row saw (-1: it does not count)
   auto rows_of = [&](int r0, bf16x8 (&q)[NS], float (&to)[2][32]) __attribute__((always_inline)) {
     const int r = min(r0 + l32, R - 1), i = r / p.G, head = g * p.G + (r - i * p.G);
     const int node = p.path ? p.path[(int64_t)b * p.max_rows + i] : i;
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
       minus = -lse * kLog2e;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (half == 0) to[0][l32] = counts ? minus : -INFINITY, to[1][l32] = __int_as_float(old + i);
+    if (half == 0) to[0][l32] = counts ? minus : -INFINITY, to[1][l32] = __int_as_float(counts ? old + i : -1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   // a block's products with a block of rows, as weights, added to this lane's key's sum (of this half's rows)
@@ -146,17 +146,25 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
     f32x16 x = {};
 #pragma unroll
     for (int s = 0; s < NS; ++s) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[s], x, 0, 0, 0);
+    const float before = sum;
+    auto add = [&](bool select) __attribute__((always_inline)) {
+      sum = before;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const f32x4 l = *(const f32x4 *)(to[0] + 8 * c + 4 * half);
-      f32x4 last = {};
-      if (!all_seen) last = *(const f32x4 *)(to[1] + 8 * c + 4 * half);
+      for (int c = 0; c < 4; ++c) {
+        const f32x4 l = *(const f32x4 *)(to[0] + 8 * c + 4 * half);
+        f32x4 last = {};
+        if (select) last = *(const f32x4 *)(to[1] + 8 * c + 4 * half);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(x[c * 4 + e], p.scale_log2, l[e]));
-        sum += all_seen || key + l32 <= __float_as_int(last[e]) ? w : 0.f;
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[c * 4 + e], p.scale_log2, l[e]));
+          sum += !select || key + l32 <= __float_as_int(last[e]) ? w : 0.f;
+        }
       }
-    }
+    };
+    add(!all_seen);
+    // Rows that do not count have operands of 0 and -inf for minus their log-sum-exp, which gives 0 except with a key that is not finite
+    // (0 * inf; 4-bit rows have none): such a block is gone through again, row by row.
+    if (KIND != TVA_ROWS_E2M1 && all_seen && __any(sum != sum)) add(true);
   };
 
   bf16x8 q[NS];
