@@ -57,11 +57,25 @@ def _lib():
     return lib
 
 
-def _whole(**tensors) -> None:
-    """What is passed as an address and sizes alone is packed."""
+_dtypes = {}  # names -> torch's types, looked up once
+
+
+def _is(types, t, name: str) -> None:
+    known = _dtypes.get(types)
+    if known is None:
+        import torch
+        known = _dtypes[types] = tuple(getattr(torch, n) for n in types)
+    if t.dtype not in known:
+        raise ValueError(f"{name} is {t.dtype}, not {' or '.join(types)}")
+
+
+def _typed(types, **tensors) -> None:
+    """What is passed as an address alone has the type that the kernels read and write, and is packed."""
     for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} is not contiguous")
+        if t is not None:
+            _is(types, t, name)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} is not contiguous")
 
 
 def _indices(**tensors) -> None:
@@ -70,11 +84,51 @@ def _indices(**tensors) -> None:
             raise ValueError(f"{name} is a contiguous int32 tensor")
 
 
+def _at_least(count: int, **tensors) -> None:
+    """One entry per sequence (or `count` in all)."""
+    for name, t in tensors.items():
+        if t is not None and t.numel() < count:
+            raise ValueError(f"{name} has {t.numel()} entries, not {count}")
+
+
+def _one_device(*tensors) -> None:
+    first = None
+    for t in tensors:
+        if t is None:
+            continue
+        if first is None:
+            first = t.device
+        elif t.device != first:
+            raise ValueError("tensors lie on different devices")
+
+
+def _fits(cache, B: int, *tensors) -> None:
+    """The sequences' places are there, and everything lies on one device (of a cache made here; a copy is not looked into)."""
+    k = getattr(cache, "_keep", ())
+    _one_device(*tensors, *k)
+    if k:
+        cu_L, page_table = k[4:6]
+        if cu_L is not None and cu_L.numel() < B + 1:
+            raise ValueError(f"cu_L has {cu_L.numel()} entries for {B} sequences")
+        if page_table is not None and page_table.shape[0] < B:
+            raise ValueError(f"page_table has {page_table.shape[0]} rows for {B} sequences")
+
+
+_ROW_TYPES = {ROWS_BF16: ("bfloat16",), ROWS_E4M3: ("uint8", "float8_e4m3fn"), ROWS_E2M1: ("uint8",)}
+
+
 def make_cache(*, k, v=None, k_row_scale=None, v_row_scale=None, kind: int = ROWS_E2M1, cu_L=None, page_table=None, page_size: int = 0,
                strides=(0, 0, 0), k_scale: float = 1.0, v_scale: float = 1.0) -> Cache:
     """A cache's tensors, any shape: where a row lies is said by the strides (elements of page, token, head; 0 = packed
     token-major).  v may be left out where only K is read (evict.key_weights)."""
     _indices(cu_L=cu_L, page_table=page_table)
+    if page_table is not None and page_table.dim() != 2:
+        raise ValueError("page_table has a row per sequence")
+    rows = _ROW_TYPES.get(int(kind))  # (another kind: the library refuses it)
+    for name, t, types in (("k", k, rows), ("v", v, rows), ("k_row_scale", k_row_scale, ("uint8",)), ("v_row_scale", v_row_scale, ("bfloat16",))):
+        if t is not None and types is not None:
+            _is(types, t, name)
+    _one_device(k, v, k_row_scale, v_row_scale, cu_L, page_table)
     c = Cache()
     c.kind, c.page_size, c.max_pages = int(kind), int(page_size), int(page_table.shape[1]) if page_table is not None else 0
     c.k_scale, c.v_scale = float(k_scale), float(v_scale)
@@ -90,12 +144,17 @@ def make_cache(*, k, v=None, k_row_scale=None, v_row_scale=None, kind: int = ROW
 def make_rows_args(*, k_rows, v_rows, cu_T, L, cache: Cache, max_rows: int, path=None, path_len=None, L_out=None, err_flag=None,
                    n_layers: int = 0, layer_stride_cache: int = 0, layer_stride_rows: int = 0) -> RowsArgs:
     """k_rows, v_rows: bf16 [.., Hkv, D] (with n_layers > 1 the first layer's lead, the others layer_stride_rows elements further on)."""
-    _whole(k_rows=k_rows, v_rows=v_rows)
+    _typed(("bfloat16",), k_rows=k_rows, v_rows=v_rows)
     _indices(cu_T=cu_T, L=L, path=path, path_len=path_len, L_out=L_out, err_flag=err_flag)
     a = RowsArgs()
     a.B, a.Hkv, a.D, a.max_rows = cu_T.numel() - 1, int(k_rows.shape[-2]), int(k_rows.shape[-1]), int(max_rows)
     if path is not None and int(path.shape[1]) != a.max_rows:
         raise ValueError("max_rows is the row length of path")
+    if tuple(v_rows.shape) != tuple(k_rows.shape):
+        raise ValueError("v_rows has the shape of k_rows")
+    _at_least(a.B, L=L, path_len=path_len, L_out=L_out)
+    _at_least(a.B * a.max_rows, path=path)
+    _fits(cache, a.B, k_rows, v_rows, cu_T, L, path, path_len, L_out, err_flag)
     a.cu_T, a.L, a.path, a.path_len, a.k_rows, a.v_rows = _p(cu_T), _p(L), _p(path), _p(path_len), _p(k_rows), _p(v_rows)
     a.cache, a.L_out, a.err_flag = cache, _p(L_out), _p(err_flag)
     a.n_layers, a.layer_stride_cache, a.layer_stride_rows = int(n_layers), int(layer_stride_cache), int(layer_stride_rows)
@@ -125,13 +184,33 @@ def load(*, stream=None, **kw) -> None:
 
 def make_attn_args(*, q, k_tree, v_tree, cache: Cache, cu_T, L, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
                    lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0) -> Attn4Args:
-    """q bf16 [sum_T, Hq, D], k_tree / v_tree bf16 [sum_T, Hkv, D], out bf16 like q, lse fp32 [sum_T, Hq] or None."""
-    _whole(q=q, k_tree=k_tree, v_tree=v_tree, anc_mask=anc_mask, out=out, lse=lse, workspace=workspace)
+    """q bf16 [sum_T, Hq, D], k_tree / v_tree bf16 [sum_T, Hkv, D], out bf16 like q, lse fp32 [sum_T, Hq] or None (either may have
+    more rows, which are left alone)."""
+    _typed(("bfloat16",), q=q, k_tree=k_tree, v_tree=v_tree, out=out)
+    _typed(("float32",), lse=lse)
+    _typed(("int64", "uint64"), anc_mask=anc_mask)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace is not contiguous")
     _indices(cu_T=cu_T, L=L, parent=parent)
+    shape, tree = q.shape, k_tree.shape
+    if len(shape) != 3 or len(tree) != 3 or tree[0] < shape[0] or tree[2] != shape[2] or v_tree.shape != tree:
+        raise ValueError("q is [sum_T, Hq, D], k_tree and v_tree are [sum_T, Hkv, D]")
+    rows = shape[0]
+    if out is not None and (out.shape[0] < rows or out.shape[1:] != shape[1:]):
+        raise ValueError("out has a row for every row of q")
+    if lse is not None and (lse.dim() != 2 or lse.shape[0] < rows or lse.shape[1] != shape[1]):
+        raise ValueError("lse has a number for every row and head of q")
+    if anc_mask is not None and (anc_mask.dim() != 2 or anc_mask.shape[0] < rows):
+        raise ValueError("anc_mask has a row for every row of q")
+    if parent is not None and parent.numel() < rows:
+        raise ValueError("parent has an entry for every row of q")
+    B = cu_T.numel() - 1
+    _at_least(B, L=L)
+    _fits(cache, B, q, k_tree, v_tree, anc_mask, out, lse, workspace, cu_T, L, parent)
     a = Attn4Args()
-    a.B = cu_T.numel() - 1
-    a.sum_T, a.Hq, a.D = (int(s) for s in q.shape)
-    a.Hkv = int(k_tree.shape[1])
+    a.B = B
+    a.sum_T, a.Hq, a.D = shape
+    a.Hkv = tree[1]
     a.max_T, a.max_L, a.num_splits, a.plan_rows = int(max_T), int(max_L), int(num_splits), int(plan_rows)
     a.mask_words = int(anc_mask.shape[1]) if anc_mask is not None else max(1, (int(max_T) + 63) // 64)
     a.scale = float(scale)

@@ -7,7 +7,7 @@ import ctypes
 
 from . import binding
 from .binding import _p
-from .cache4 import Cache, _indices, _whole
+from .cache4 import Cache, _at_least, _fits, _indices, _one_device, _typed
 
 _ready = False
 
@@ -52,7 +52,8 @@ def _lib():
 def make_key_weight_args(*, q, lse, cache: Cache, cu_T, L, weight, max_rows: int, max_L: int, scale: float, path=None, path_len=None,
                          pos=None, first_pos=None) -> KeyWeightArgs:
     """q bf16 [sum_T, Hq, D] and lse fp32 [sum_T, Hq] of a step's attention; weight fp32 (and pos int32) [B, Hkv, ld]."""
-    _whole(q=q, lse=lse, weight=weight)
+    _typed(("bfloat16",), q=q)
+    _typed(("float32",), lse=lse, weight=weight)
     _indices(cu_T=cu_T, L=L, path=path, path_len=path_len, pos=pos, first_pos=first_pos)
     a = KeyWeightArgs()
     a.B, a.Hq, a.Hkv, a.D = cu_T.numel() - 1, int(q.shape[1]), int(weight.shape[1]), int(q.shape[2])
@@ -61,6 +62,13 @@ def make_key_weight_args(*, q, lse, cache: Cache, cu_T, L, weight, max_rows: int
         raise ValueError("max_rows is the row length of path")
     if pos is not None and tuple(pos.shape) != tuple(weight.shape):
         raise ValueError("pos has the shape of weight")
+    if tuple(lse.shape) != tuple(q.shape[:2]):
+        raise ValueError("lse has a number for every row and head of q")
+    if weight.dim() != 3 or weight.shape[0] < a.B:
+        raise ValueError("weight is [B, Hkv, ld]")
+    _at_least(a.B, L=L, path_len=path_len, first_pos=first_pos)
+    _at_least(a.B * a.max_rows, path=path)
+    _fits(cache, a.B, q, lse, weight, pos, cu_T, L, path, path_len, first_pos)
     a.cu_T, a.path, a.path_len, a.L, a.q, a.lse = _p(cu_T), _p(path), _p(path_len), _p(L), _p(q), _p(lse)
     a.cache, a.weight, a.pos, a.first_pos, a.ld = cache, _p(weight), _p(pos), _p(first_pos), int(weight.shape[2])
     # the struct holds raw addresses: keep the tensors alive as long as it lives
@@ -70,11 +78,15 @@ def make_key_weight_args(*, q, lse, cache: Cache, cu_T, L, weight, max_rows: int
 
 def make_select_args(*, weight, L, keep, max_L: int, src, L_out=None, n_first: int = 0, newest=None, pos=None) -> SelectArgs:
     """weight fp32 (and pos int32) [n_layers, B, H, ld] or [B, H, ld], src int32 likewise with ld_src."""
-    _whole(weight=weight)
+    _typed(("float32",), weight=weight)
     _indices(L=L, keep=keep, src=src, L_out=L_out, newest=newest, pos=pos)
     a = SelectArgs()
     if tuple(src.shape[:-1]) != tuple(weight.shape[:-1]) or (pos is not None and tuple(pos.shape) != tuple(weight.shape)):
         raise ValueError("weight, pos and src have the same rows")
+    if weight.dim() not in (3, 4):
+        raise ValueError("weight is [B, H, ld] or [n_layers, B, H, ld]")
+    _at_least(int(weight.shape[-3]), L=L, keep=keep, newest=newest, L_out=L_out)
+    _one_device(weight, pos, src, L, keep, newest, L_out)
     a.n_layers = int(weight.shape[0]) if weight.dim() == 4 else 1
     a.B, a.H, a.max_L, a.n_first = int(weight.shape[-3]), int(weight.shape[-2]), int(max_L), int(n_first)
     a.L, a.keep, a.newest, a.weight, a.pos = _p(L), _p(keep), _p(newest), _p(weight), _p(pos)
@@ -86,7 +98,7 @@ def make_select_args(*, weight, L, keep, max_L: int, src, L_out=None, n_first: i
 def make_move_args(*, src, n, cache: Cache, Hkv: int, D: int, max_keep: int, weight=None, pos=None, layer_stride_cache: int = 0,
                    err_flag=None) -> MoveArgs:
     """src int32 [n_layers, B, H, ld_src] or [B, H, ld_src] (H = Hkv, or 1: shared by the heads), n: select's L_out."""
-    _whole(weight=weight)
+    _typed(("float32",), weight=weight)
     _indices(src=src, n=n, pos=pos, err_flag=err_flag)
     a = MoveArgs()
     for t in (weight, pos):
@@ -94,6 +106,10 @@ def make_move_args(*, src, n, cache: Cache, Hkv: int, D: int, max_keep: int, wei
             raise ValueError("src, weight and pos have the same rows")
     if weight is not None and pos is not None and weight.shape[-1] != pos.shape[-1]:
         raise ValueError("pos has the shape of weight")
+    if src.dim() not in (3, 4):
+        raise ValueError("src is [B, H, ld_src] or [n_layers, B, H, ld_src]")
+    _at_least(int(src.shape[-3]), n=n)
+    _fits(cache, int(src.shape[-3]), src, n, weight, pos, err_flag)
     a.n_layers = int(src.shape[0]) if src.dim() == 4 else 1
     a.B, a.H, a.Hkv, a.D, a.max_keep = int(src.shape[-3]), int(src.shape[-2]), int(Hkv), int(D), int(max_keep)
     a.n, a.src, a.ld_src, a.cache, a.layer_stride_cache = _p(n), _p(src), int(src.shape[-1]), cache, int(layer_stride_cache)
