@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   typedef FourCfg<D> C;
   constexpr int WK = kWaves / WM;
   // Remainders in every tile, or in a block of their own where some row needs them.  In every tile where several 32-row blocks share the
-  // keys, which mostly is work of a few tiles per wave that need them all (one sequence of 2048 keys, 60 nodes: 15.4 us, 16.6 with the
+  // keys, which is work of a few tiles per wave that need them all, or of three blocks (one sequence of 2048 keys, 60 nodes: 15.4 us, 16.6 with the
   // block, 14.5 without remainders); else few tiles need them (64 sequences of 4096 .. 16384 keys, 8 nodes: 182 us, 165, 160; 4 of
   // 16384 .. 32768, 48 nodes: 141 us, 124, 117).
   constexpr bool ALWAYS = WM == 1 && !NT;
@@ -791,11 +791,14 @@ struct FourPlan {
   int WM, blocks, group, groups, parts;
 };
 // 32-row workgroups while there is little work and one round of them holds it: their four waves split the keys, which costs no partial
-// results (one sequence of 2048 keys, 60 nodes: 14.8 us with 32 rows, 19.4 with 64, 25.5 with 128; but 26 sequences of 7 keys, 64
-// heads, 64 nodes 72 us with 32 rows, 42 with 128).  Else as many rows as divide the row groups without waste, so
-// that fewer workgroups read the same keys (4 sequences of 16384 .. 32768, 48 nodes, six groups: 64 rows 119 us, 128 rows 147).
-// Long work of several long sequences is dealt out over two workgroups per CU (a part of a sequence costs about four tiles of its own); a sequence by itself over one (the case above with 256
-// workgroups 14.8 us, with 512 18.5), and one run at most is a round short of a workgroup rather than one too many.
+// results (one sequence of 2048 keys, 56 nodes: 14.9 us with 32 rows, 17.2 with 64, 22.0 with 128; but 26 sequences of 7 keys, 64
+// heads, 64 nodes 76 us with 32 rows, 43 with 128).  Else as many rows as divide the row groups without waste, so that fewer workgroups
+// read the same keys, and 64 rows for an odd number from five on, which leaves one wave idle (4 sequences of 16384 .. 32768 keys, four heads
+// to a KV head, with 32 / 64 / 128 rows: 24 nodes, three groups, 80.6 / 100.2 / 90.9 us; 48, six, 140 / 123 / 148; 56, seven, 157 / 149 /
+// 155; 66, nine, 191 / 181 / 208; 80, ten, 217 / 188 / 215; 100, thirteen, 301 / 242 / 260; 112, fourteen, 308 / 246 / 269).
+// Long work of several long sequences is dealt out over two workgroups per CU (a part of a sequence costs about four tiles of its own);
+// a sequence by itself over one (the first case with 256 workgroups 14.8 us, with 512 18.5, before remainders), and one run at most is a
+// round short of a workgroup rather than one too many.
 void plan_four(const tva_attn4_args *a, FourPlan *pl) {
   constexpr int kSlots = 256, kTogether = 6, kLong = 32;
   const int G = a->Hq / a->Hkv;
@@ -803,7 +806,7 @@ void plan_four(const tva_attn4_args *a, FourPlan *pl) {
   const int tiles = (a->max_L + 63) / 64 + (a->max_T + 63) / 64;
   const int64_t pairs = (int64_t)a->B * a->Hkv;
   if (a->plan_rows) pl->WM = a->plan_rows / 32;
-  else pl->WM = groups == 1 || (pairs * groups <= 2 * kSlots && pairs * groups * tiles <= 8 * 2048) ? 1 : groups % 4 == 0 || groups > 8 ? 4 : groups % 2 == 0 ? 2 : groups == 3 ? 4 : 1;
+  else pl->WM = groups == 1 || (pairs * groups <= 2 * kSlots && pairs * groups * tiles <= 8 * 2048) ? 1 : groups == 3 ? 1 : groups % 4 == 0 ? 4 : 2;
   const int WK = kWaves / pl->WM;
   pl->blocks = (int)((groups + pl->WM - 1) / pl->WM);
   const int64_t base = (int64_t)a->Hkv * pl->blocks;
