@@ -282,10 +282,10 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
   return any;
 }
 
-template <bool NT>
-__device__ __forceinline__ u32x4 read_once(const u32x4 *p) {
-  if constexpr (NT) return __builtin_nontemporal_load(p);
-  else return *p;
+template <bool ONCE>
+__device__ __forceinline__ u32x4 read16(const char *p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4 *)p);
+  else return *(const u32x4 *)p;
 }
 
 template <int D>
@@ -314,17 +314,21 @@ struct FourCfg {
 // Grid: KV head (fastest: with 8 heads one per XCD), block of WM * 32 query rows, run of tiles.  The four waves are WM row groups x
 // 4 / WM key groups; every (4 / WM)th tile of a run's part of a sequence belongs to a key group.
 // PG: 0 dense, 1 paged, 2 paged with pages of whole tiles (one table entry per tile, and as in the dense form addresses that are a
-// scalar and a lane's offset).  NT: one block of rows reads the keys, once.  (64 sequences of 4096 .. 16384 keys, 8 nodes 160 -> 154 us; where
-// blocks share them, 4 sequences of 16384 .. 32768, 48 nodes in two blocks, 147 -> 211.)
-template <int D, int WM, int PG, bool NT>
+// scalar and a lane's offset).
+// FORM kAlways: remainders in every tile, not in a block of their own where some row needs them.  So where several 32-row blocks share the
+// keys, which is work of a few tiles per wave that need them all, or of three blocks (one sequence of 2048 keys, 60 nodes: 15.4 us, 16.6
+// with the block, 14.5 without remainders); else few tiles need them (64 sequences of 4096 .. 16384 keys, 8 nodes: 182 us, 165, 160; 4
+// of 16384 .. 32768, 48 nodes: 141 us, 124, 117).
+// FORM kOnce: keys are read by nontemporal loads, where one block of rows reads them, a head's rows lie side by side and all of them are
+// more than the last-level cache holds (64 sequences of 4096 .. 16384 keys, 8 nodes, head-major: 167 -> 164 us; 4 of 16384 .. 32768,
+// which it holds, 40 -> 42; heads of a token-major cache share lines: 250 -> 306, 16 sequences of 2048 .. 4096 keys 34 -> 54).
+enum { kPlain, kAlways, kOnce };
+constexpr int64_t kLastLevel = 256ll << 20;  // bytes
+template <int D, int WM, int PG, int FORM>
 __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
   typedef FourCfg<D> C;
   constexpr int WK = kWaves / WM;
-  // Remainders in every tile, or in a block of their own where some row needs them.  In every tile where several 32-row blocks share the
-  // keys, which is work of a few tiles per wave that need them all, or of three blocks (one sequence of 2048 keys, 60 nodes: 15.4 us, 16.6 with the
-  // block, 14.5 without remainders); else few tiles need them (64 sequences of 4096 .. 16384 keys, 8 nodes: 182 us, 165, 160; 4 of
-  // 16384 .. 32768, 48 nodes: 141 us, 124, 117).
-  constexpr bool ALWAYS = WM == 1 && !NT;
+  constexpr bool ALWAYS = FORM == kAlways, ONCE = FORM == kOnce;
   __shared__ __align__(16) unsigned char lds[C::LDS];
   const int g = blockIdx.x, which = blockIdx.z / p.parts, run = blockIdx.z - which * p.parts;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -398,7 +402,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
         const uint32_t row = row_of(kb * 32 + (ln & 31));
         const char *from = byte_of(p.c.k, row, C::RB, hf * (C::RB / 2));
 #pragma unroll
-        for (int i = 0; i < C::KL; ++i) kx[kb][i] = read_once<NT>((const u32x4 *)(from + i * 16));
+        for (int i = 0; i < C::KL; ++i) kx[kb][i] = read16<ONCE>(from + i * 16);
         if constexpr (D == 128) ks[kb] = *(const uint16_t *)byte_of(p.c.k_row_scale, row, 4, hf * 2);
         else ks[kb] = *(const uint8_t *)byte_of(p.c.k_row_scale, row, 2, hf);
       }
@@ -406,7 +410,7 @@ __global__ void __launch_bounds__(256, 2) four_bit_kernel(const FourParams p) {
     auto fetch_v = [&](int tile) __attribute__((always_inline)) {
       const int ln = afresh(tile);
 #pragma unroll
-      for (int i = 0; i < C::CH; ++i) vx[i] = read_once<NT>((const u32x4 *)byte_of(p.c.v, row_of(i * C::RPL + ln / C::CH), C::RB, (ln % C::CH) * 16));
+      for (int i = 0; i < C::CH; ++i) vx[i] = read16<ONCE>(byte_of(p.c.v, row_of(i * C::RPL + ln / C::CH), C::RB, (ln % C::CH) * 16));
       if constexpr (PG == 1) vs = *(const uint16_t *)(p.c.v_row_scale + (uint64_t)rs * 2);
       else vs = *(const uint16_t *)byte_of(p.c.v_row_scale, row_of(ln), 2, 0);
     };
@@ -923,20 +927,22 @@ int tva_tree_verify_attn_4bit(const tva_attn4_args *a, void *stream) {
   const dim3 grid(a->Hkv, pl.blocks, pl.groups * pl.parts);
   const hipStream_t st = (hipStream_t)stream;
   const int pg = !a->cache.page_table ? 0 : a->cache.page_size % 64 ? 1 : 2;
+  const bool once = p.c.stride_tok == 1 && (int64_t)a->B * a->max_L * a->Hkv * (a->D + a->D / 32 + 2) > kLastLevel;
   (void)hipGetLastError();
   auto launch = [&](auto d, auto wm) {
     constexpr int D = decltype(d)::value, WM = decltype(wm)::value;
-    auto form = [&](auto nt) {
-      constexpr bool NT = decltype(nt)::value;
-      if (pg == 0) hipLaunchKernelGGL((four_bit_kernel<D, WM, 0, NT>), grid, dim3(256), 0, st, p);
-      else if (pg == 1) hipLaunchKernelGGL((four_bit_kernel<D, WM, 1, NT>), grid, dim3(256), 0, st, p);
-      else hipLaunchKernelGGL((four_bit_kernel<D, WM, 2, NT>), grid, dim3(256), 0, st, p);
+    auto form = [&](auto f) {
+      constexpr int FORM = decltype(f)::value;
+      if (pg == 0) hipLaunchKernelGGL((four_bit_kernel<D, WM, 0, FORM>), grid, dim3(256), 0, st, p);
+      else if (pg == 1) hipLaunchKernelGGL((four_bit_kernel<D, WM, 1, FORM>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((four_bit_kernel<D, WM, 2, FORM>), grid, dim3(256), 0, st, p);
     };
     if constexpr (WM == 1) {
-      if (pl.blocks == 1) form(std::true_type{});
-      else form(std::false_type{});
+      if (pl.blocks > 1) form(std::integral_constant<int, kAlways>{});
+      else if (once) form(std::integral_constant<int, kOnce>{});
+      else form(std::integral_constant<int, kPlain>{});
     } else {
-      form(std::false_type{});
+      form(std::integral_constant<int, kPlain>{});
     }
     if (pl.parts > 1 && hipPeekAtLastError() == hipSuccess)
       hipLaunchKernelGGL(join_kernel<D>, dim3(a->Hkv, (p.rows + 1024 / D - 1) / (1024 / D), a->B), dim3(256), 0, st, p, WM * 32);

@@ -36,3 +36,14 @@ def test_the_library_deals_out_long_trees_by_itself(torch):
     sizes, lengths = _batch(rng, 40, 48)
     args, *_ = _attend(torch, rng, (8, 2, 128), sizes, lengths, 16)
     assert cache4.plan_splits(args) > 20
+
+
+@pytest.mark.parametrize("page", [0, 5, 16, 64])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
+def test_heads_kept_together_in_more_than_the_last_level_cache_holds(torch, heads, page):
+    """One block of rows per head, head-major, and a bound of the lengths by which the cache passes 256 MB: keys are read another way then."""
+    rng = np.random.default_rng(heads[0] + page)
+    assert 3 * (1 << 20) * heads[1] * heads[2] > 256 << 20
+    for sizes, lengths in (([1, 1, 1], [700, 0, 64]), ([5, 0, 8], [130, 64, 2100]), ([2, 3, 1], [1, 63, 65])):
+        _attend(torch, rng, heads, sizes, lengths, page, True, max_L=1 << 20)
+    _attend(torch, rng, heads, [7], [900], page, True, max_L=1 << 22, splits=3)
