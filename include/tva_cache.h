@@ -37,6 +37,8 @@ typedef enum {
  * token-major.  BF16: multiples of 8, E4M3: of 16, E2M1: of D (a row's scales are found by element / D).
  * Positions are below 2^30; E2M1 row numbers (element / D) below 2^32, and stride_tok below 2^25 (2^24 bytes).
  * Head-major ([.., Hkv, page_size, D]: stride_tok = D, stride_head = page_size*D) keeps a head's keys together.
+ * tva_cache_store and tva_evict_move write in place: a page (or row) that they reach belongs to one sequence.  Sequences that
+ * share a prefix's pages are given pages of their own before either is called for those positions; the other calls only read.
  */
 typedef struct tva_cache {
   int32_t kind; /* a tva_row_kind */
@@ -127,15 +129,14 @@ size_t tva_sizeof_attn4_args(void);
 
 /*
  * The attention that cached keys receive, added up: what eviction goes by.  Called after the attention and the commit
- * of a step.  Sequence b's n_b newest tokens (rows as in tva_rows_args: an accepted path, or all of cu_T) sit at positions
- * L[b]-n_b .. L[b]-1 of its cache, and row i of them saw the positions t <= L[b]-n_b+i.  With q and lse of those rows (the
+ * of a step.  Sequence b's n_b newest tokens (rows as in tva_rows_args: an accepted path, or all of cu_T, max_rows at most, as
+ * many as tva_cache_store took) sit at positions L[b]-n_b .. L[b]-1 of its cache, and row i of them saw the positions t <= L[b]-n_b+i.  With q and lse of those rows (the
  * attention's input and output), for every KV head g and position t
  *     weight[b,g,t] = (t < L[b]-n_b ? weight[b,g,t] : 0) + sum over rows i that saw t, query heads h of g,
  *                                                          exp(scale * <q[i,h,:], K[t,g,:]> - lse[i,h])
  * so what the new tokens' entries held before does not matter.  A row whose lse is -inf adds nothing.  Entries from L[b]
  * on are left as they are.  pos, if given, gets first_pos[b] + i at the new tokens' entries: the age that eviction can
- * protect.  At most max_rows rows of a sequence are taken (the first ones); a path entry that is not one of the
- * sequence's rows adds nothing.  Sums are fp32, in an order that does not change from call to call.
+ * protect.  A path entry that is not one of the sequence's rows adds nothing.  Sums are fp32, in an order that does not change from call to call.
  * Each head of each sequence has ld entries (>= every L[b]) in weight and pos.  max_L truncates as in tva_args.
  */
 typedef struct tva_key_weight_args {
@@ -164,7 +165,9 @@ size_t tva_sizeof_key_weight_args(void);
  * Which slots stay.  Each of the H weight rows of a sequence (one per KV head; or H = 1 for a choice that all heads share)
  * keeps n = min(keep[b], L[b]) of its first L[b] slots: first the protected ones, then by weight, largest first; among
  * equal ones the lower slot.  Protected: slots below n_first, and those whose age counts as new: pos[slot] >= newest[b]
- * (without pos: slot >= newest[b]; without newest: none).  A NaN weight is below all others; -0 equals 0.
+ * (without pos: slot >= newest[b]; without newest: none).  Protected slots are equals: if there are more of them than n, the
+ * lower ones stay, whatever their age, so keep is no less than n_first and the new ones together where these are meant to
+ * stay.  A NaN weight is below all others; -0 equals 0.
  *
  * Softmax does not depend on the order of the keys, so nothing is shifted: kept slots below n stay where they are, and
  * the m-th gap below n (in ascending order) is given the m-th kept slot from n on.  src[.., j] for j < n is the slot whose

@@ -94,6 +94,12 @@ inline int view_of(const tva_cache &a, int Hkv, int D, bool need_v, CacheView *c
   return TVA_OK;
 }
 
+// A lane's number and that of the lane 32 further on, added
+__device__ __forceinline__ float half_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ float exponent_byte(uint32_t x) { return __uint_as_float(x << 23); }  // 2^(x - 127), x of 1 .. 254
 
 // The eight codes of a word -> bf16 values times s (a power of two, so exact).

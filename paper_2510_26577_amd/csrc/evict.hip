@@ -38,11 +38,6 @@ struct WeighParams {
   float scale_log2;
 };
 
-__device__ __forceinline__ float half_sum(float x) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // Four consecutive E4M3 bytes' pairs -> bf16 (exact)
 __device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, true);
