@@ -129,14 +129,15 @@ size_t tva_sizeof_attn4_args(void);
 
 /*
  * The attention that cached keys receive, added up: what eviction goes by.  Called after the attention and the commit
- * of a step.  Sequence b's n_b newest tokens (rows as in tva_rows_args: an accepted path, or all of cu_T, max_rows at most, as
- * many as tva_cache_store took) sit at positions L[b]-n_b .. L[b]-1 of its cache, and row i of them saw the positions t <= L[b]-n_b+i.  With q and lse of those rows (the
- * attention's input and output), for every KV head g and position t
+ * of a step.  Sequence b's n_b newest tokens (rows as in tva_rows_args: an accepted path, or all of cu_T; max_rows at most,
+ * as many as tva_cache_store took) sit at positions L[b]-n_b .. L[b]-1 of its cache, and row i of them saw the positions
+ * t <= L[b]-n_b+i.  With q and lse of those rows (the attention's input and output), for every KV head g and position t
  *     weight[b,g,t] = (t < L[b]-n_b ? weight[b,g,t] : 0) + sum over rows i that saw t, query heads h of g,
  *                                                          exp(scale * <q[i,h,:], K[t,g,:]> - lse[i,h])
- * so what the new tokens' entries held before does not matter.  A row whose lse is -inf adds nothing.  Entries from L[b]
- * on are left as they are.  pos, if given, gets first_pos[b] + i at the new tokens' entries: the age that eviction can
- * protect.  A path entry that is not one of the sequence's rows adds nothing.  Sums are fp32, in an order that does not change from call to call.
+ * so what the new tokens' entries held before does not matter.  A row whose lse is -inf adds nothing, and neither does a path
+ * entry that is not one of the sequence's rows.  Entries from L[b] on are left as they are.  pos, if given, gets
+ * first_pos[b] + i at the new tokens' entries: the age that eviction can protect.  Sums are fp32, in an order that does not
+ * change from call to call.
  * Each head of each sequence has ld entries (>= every L[b]) in weight and pos.  max_L truncates as in tva_args.
  */
 typedef struct tva_key_weight_args {

@@ -110,30 +110,23 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) entry[u] = find.entry(p.c, own(key0 + 32 * (AHEAD + u)));
 
-  const int R = n * p.G;
+  const int R = T > 0 ? n * p.G : 0;  // (a sequence without rows has none to read, and the last one's would lie behind the tensors)
   // rows r0 .. r0+31: query operand (a row per lane), and in LDS minus log-sum-exp and the last position the row saw (-1: it does not count)
   auto rows_of = [&](int r0, bf16x8 (&q)[NS], float (&to)[2][32]) __attribute__((always_inline)) {
     const int r = min(r0 + l32, R - 1), i = r / p.G, head = g * p.G + (r - i * p.G);
     const int node = p.path ? p.path[(int64_t)b * p.max_rows + i] : i;
     const bool there = node >= 0 && node < T;
-    bool counts = false;
-    float minus = 0.f;
+    const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
+    const float lse = p.lse[row];
+    const bool counts = there && r0 + l32 < R && lse != -INFINITY;
+    const __bf16 *from = p.q + row * D;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) q[s] = bf16x8{};
-    if (T > 0) {  // (a sequence without rows has none to read, and the last one's would lie behind the tensors)
-      const int64_t row = (int64_t)(t0 + (there ? node : 0)) * p.Hq + head;
-      const float lse = p.lse[row];
-      counts = there && r0 + l32 < R && lse != -INFINITY;
-      const __bf16 *from = p.q + row * D;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        q[s] = *(const bf16x8 *)(from + (KIND == TVA_ROWS_BF16 ? s * 16 + half * 8 : half * (D / 2) + s * 8));
-        if (!counts) q[s] = bf16x8{};  // (whatever it holds)
-      }
-      minus = -lse * kLog2e;
+    for (int s = 0; s < NS; ++s) {
+      q[s] = *(const bf16x8 *)(from + (KIND == TVA_ROWS_BF16 ? s * 16 + half * 8 : half * (D / 2) + s * 8));
+      if (!counts) q[s] = bf16x8{};  // (whatever it holds)
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (half == 0) to[0][l32] = counts ? minus : -INFINITY, to[1][l32] = __int_as_float(counts ? old + i : -1);
+    if (half == 0) to[0][l32] = counts ? -lse * kLog2e : -INFINITY, to[1][l32] = __int_as_float(counts ? old + i : -1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   // a block's products with a block of rows, as weights, added to this lane's key's sum (of this half's rows)
@@ -163,7 +156,14 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
   };
 
   bf16x8 q[NS];
-  rows_of(0, q, lds[wave][0]);
+  if (R > 0) {
+    rows_of(0, q, lds[wave][0]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = bf16x8{};
+    if (half == 0) lds[wave][0][0][l32] = -INFINITY, lds[wave][0][1][l32] = __int_as_float(-1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
   const int first_pos = p.pos && end > old ? p.first_pos[b] : 0;
   for (int base = key0;; base += 32 * AHEAD)
 #pragma unroll
