@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(64 * kWeighWaves, D == 128 && KIND != TVA_ROWS
         }
       }
     };
-    add(!all_seen);
+    if (all_seen) add(false);
+    else add(true);
     // Rows that do not count have operands of 0 and -inf for minus their log-sum-exp, which gives 0 except with a key that is not finite
     // (0 * inf; 4-bit rows have none): such a block is gone through again, row by row.
     if (KIND != TVA_ROWS_E2M1 && all_seen && __any(sum != sum)) add(true);
