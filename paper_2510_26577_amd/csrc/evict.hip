@@ -484,7 +484,8 @@ int tva_key_weights(const tva_key_weight_args *a, void *stream) {
   p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.max_rows = a->max_rows, p.max_L = a->max_L;
   const float ks = a->cache.kind == TVA_ROWS_E4M3 && a->cache.k_scale != 0.f ? a->cache.k_scale : 1.f;
   p.scale_log2 = a->scale * ks * kLog2e;
-  // blocks per wave: as many as leave 4096 waves, at most 8 (16 x 16384 .. 32768 4-bit keys: with 4 / 8 / 16 / 32 79 / 70.6 / 71.9 / 86 us)
+  // blocks per wave: as many as leave 4096 waves, at most 8 (16 x 16384 .. 32768 4-bit keys, before blocks that all rows
+  // see had a form of their own, 66 us now: with 4 / 8 / 16 / 32 79 / 70.6 / 71.9 / 86 us)
   const int64_t all_blocks = ((int64_t)a->max_L + 31) / 32;
   p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, all_blocks * a->B * a->Hkv / 4096));
   const int64_t waves = (all_blocks + p.blocks - 1) / p.blocks * a->Hkv, groups = (waves + kWeighWaves - 1) / kWeighWaves;
