@@ -102,6 +102,12 @@ def _one_device(*tensors) -> None:
             raise ValueError("tensors lie on different devices")
 
 
+def _on_gpu(t) -> None:
+    """(All of a call's tensors lie on one device: one of them says which.)"""
+    if not t.is_cuda:
+        raise ValueError(f"tensors lie on {t.device}, not on a GPU")
+
+
 def _fits(cache, B: int, *tensors) -> None:
     """The sequences' places are there, and everything lies on one device (of a cache made here; a copy is not looked into)."""
     k = getattr(cache, "_keep", ())
@@ -174,12 +180,16 @@ def load_raw(args: RowsArgs, stream=None) -> None:
 
 def store(*, stream=None, **kw) -> None:
     """Keyword arguments of make_rows_args: bf16 rows (a prompt, or an accepted path) become 4-bit rows of the cache, in place."""
-    store_raw(make_rows_args(**kw), stream)
+    args = make_rows_args(**kw)
+    _on_gpu(kw["k_rows"])
+    store_raw(args, stream)
 
 
 def load(*, stream=None, **kw) -> None:
     """Keyword arguments of make_rows_args: the values of the cache's 4-bit rows are written to k_rows and v_rows."""
-    load_raw(make_rows_args(**kw), stream)
+    args = make_rows_args(**kw)
+    _on_gpu(kw["k_rows"])
+    load_raw(args, stream)
 
 
 def make_attn_args(*, q, k_tree, v_tree, cache: Cache, cu_T, L, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
@@ -261,6 +271,7 @@ def tree_verify_attn(q, k_tree, v_tree, cache: Cache, cu_T, L, *, max_T: int, ma
         lse = torch.empty(tuple(q.shape[:2]), dtype=torch.float32, device=q.device)
     a = make_attn_args(q=q, k_tree=k_tree, v_tree=v_tree, cache=cache, cu_T=cu_T, L=L, max_T=max_T, max_L=max_L, scale=scale, anc_mask=anc_mask,
                        parent=parent, out=out, lse=lse, workspace=workspace, num_splits=num_splits, plan_rows=plan_rows)
+    _on_gpu(q)
     ws = attn_workspace(a, q.device) if workspace is None else None
     tree_verify_attn_raw(a, stream)
     if ws is not None and stream is not None:  # it goes back to the current stream's pool: not before the work on `stream` is done

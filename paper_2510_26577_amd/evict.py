@@ -7,7 +7,7 @@ import ctypes
 
 from . import binding
 from .binding import _p
-from .cache4 import Cache, _at_least, _fits, _indices, _one_device, _typed
+from .cache4 import Cache, _at_least, _fits, _indices, _on_gpu, _one_device, _typed
 
 _ready = False
 
@@ -133,7 +133,9 @@ def move_raw(args: MoveArgs, stream=None) -> None:
 
 def key_weights(*, stream=None, **kw) -> None:
     """Keyword arguments of make_key_weight_args; weight (and pos) are brought up to date in place."""
-    key_weights_raw(make_key_weight_args(**kw), stream)
+    args = make_key_weight_args(**kw)
+    _on_gpu(kw["q"])
+    key_weights_raw(args, stream)
 
 
 def select(weight, L, keep, *, max_L: int, max_keep: int, n_first: int = 0, newest=None, pos=None, src=None, L_out=None, stream=None):
@@ -143,10 +145,14 @@ def select(weight, L, keep, *, max_L: int, max_keep: int, n_first: int = 0, newe
         src = torch.empty((*weight.shape[:-1], max(1, int(max_keep))), dtype=torch.int32, device=weight.device)
     if L_out is None:
         L_out = torch.empty(int(weight.shape[-3]), dtype=torch.int32, device=weight.device)
-    select_raw(make_select_args(weight=weight, L=L, keep=keep, max_L=max_L, src=src, L_out=L_out, n_first=n_first, newest=newest, pos=pos), stream)
+    args = make_select_args(weight=weight, L=L, keep=keep, max_L=max_L, src=src, L_out=L_out, n_first=n_first, newest=newest, pos=pos)
+    _on_gpu(weight)
+    select_raw(args, stream)
     return src, L_out
 
 
 def move(*, stream=None, **kw) -> None:
     """Keyword arguments of make_move_args; cache, weight and pos are changed in place."""
-    move_raw(make_move_args(**kw), stream)
+    args = make_move_args(**kw)
+    _on_gpu(kw["src"])
+    move_raw(args, stream)

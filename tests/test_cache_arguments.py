@@ -145,3 +145,15 @@ def test_tensors_that_are_not_packed_are_refused(which, name):
     wide = torch.zeros((*given.shape[:-1], given.shape[-1] * 2), dtype=given.dtype)[..., ::2]
     with pytest.raises(ValueError, match="not contiguous"):
         _make(which, **{name: wide})
+
+
+def test_calls_on_host_tensors_are_refused():
+    c = cache4.make_cache(**_cache())
+    attn = _attn()
+    where = [attn.pop(n) for n in ("q", "k_tree", "v_tree", "cu_T", "L")]
+    for call in (lambda: cache4.store(cache=c, **_rows()), lambda: cache4.load(cache=c, **_rows(L_out=None)),
+                 lambda: cache4.tree_verify_attn(where[0], where[1], where[2], c, where[3], where[4], **attn),
+                 lambda: evict.key_weights(cache=c, **_weigh()), lambda: evict.select(_t(B, HKV, LD), _t(B, dtype=I), _t(B, dtype=I), max_L=LD, max_keep=LD),
+                 lambda: evict.move(cache=c, **_move())):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
