@@ -235,7 +235,7 @@ def _prepare_attn(case, rng, gen):
         s["out"], s["lse"] = torch.empty((n, Hq, D), dtype=torch.bfloat16, device=DEV), torch.empty((n, Hq), dtype=torch.float32, device=DEV)
         s["args"] = chunk.make_args(q=s["q"], cache=_own_cache(s, D, case["rows"]), cu_T=s["cu_T"], L=s["L"], Hkv=Hkv, max_T=max_T, max_L=s["max_L"],
                                     scale=s["scale"], window=s["window"], n_first=s["first"], anc_mask=s["mask"], out=s["out"], lse=s["lse"])
-        s["ws"] = chunk.workspace(s["args"], DEV)
+        s["ws"] = chunk.attn_workspace(s["args"], DEV)
     return s
 
 
