@@ -22,13 +22,15 @@ VERIFY_SRC_PATH = os.path.join(_HERE, "csrc", "verify.hip")  # acceptance + comm
 DRAFT_SRC_PATH = os.path.join(_HERE, "csrc", "draft.hip")    # draft-tree expansion + subtree kernels
 CACHE4_SRC_PATH = os.path.join(_HERE, "csrc", "cache4.hip")  # 4-bit rows: store, load, attention
 EVICT_SRC_PATH = os.path.join(_HERE, "csrc", "evict.hip")    # key weights, choice of slots, moves
+ROTARY_SRC_PATH = os.path.join(_HERE, "csrc", "rotary.hip")  # rotary positions, norms of heads, append to the cache
+CHUNK_SRC_PATH = os.path.join(_HERE, "csrc", "chunk.hip")    # attention of new tokens over the cache that holds them
 PYCALL_SRC_PATH = os.path.join(_HERE, "csrc", "pycall.cpp")  # calls on tensors in native code (module _pycall)
 PYCALL_LIB_PATH = os.path.join(_HERE, "_pycall.so")
 INCLUDE_DIR = os.path.join(_ROOT, "include")
 
 TVA_OK = 0
 TVA_MAX_TREE = 128
-EXPECTED_VERSION = 7
+EXPECTED_VERSION = 8
 # tva_shape (include/tva.h): workgroup shapes a caller may name in tva_args.plan_shape
 SHAPE_AUTO, SHAPE_R32_W2, SHAPE_R64_W4, SHAPE_R64_W4_DEEP, SHAPE_R128_W8, SHAPE_R256_W8 = range(6)
 SHAPES = (SHAPE_R32_W2, SHAPE_R64_W4, SHAPE_R64_W4_DEEP, SHAPE_R128_W8, SHAPE_R256_W8)
@@ -45,13 +47,13 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17",
 
 
 def build_library(verbose: bool = False, timeline: bool = False) -> str:
-    """Compile csrc/tva.hip, csrc/verify.hip, csrc/draft.hip, csrc/cache4.hip and csrc/evict.hip (gfx950 kernels + their
+    """Compile csrc/tva.hip, csrc/verify.hip, csrc/draft.hip, csrc/cache4.hip, csrc/evict.hip, csrc/rotary.hip and csrc/chunk.hip (gfx950 kernels + their
     C ABI) and csrc/cast.cpp (host logic) into libtva.so (in-tree); timeline=True: the instrumented build libtva_timeline.so
     (paper_2510_26577_amd/timeline.py) instead."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out = TIMELINE_LIB_PATH if timeline else LIB_PATH
     cmd = [hipcc, *HIPCC_FLAGS, *(["-DTVA_TIMELINE"] if timeline else []), "-I", INCLUDE_DIR, "-shared", "-fPIC", "-o", out,
-           SRC_PATH, VERIFY_SRC_PATH, DRAFT_SRC_PATH, CACHE4_SRC_PATH, EVICT_SRC_PATH, CAST_SRC_PATH]
+           SRC_PATH, VERIFY_SRC_PATH, DRAFT_SRC_PATH, CACHE4_SRC_PATH, EVICT_SRC_PATH, ROTARY_SRC_PATH, CHUNK_SRC_PATH, CAST_SRC_PATH]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     lines = [l for l in res.stdout.splitlines() if "is not a recognized feature" not in l]
     if verbose or res.returncode:
@@ -117,6 +119,9 @@ VERIFY_EXPORTS = ("tva_accept_greedy", "tva_accept_greedy_filled", "tva_accept_s
 CACHE_EXPORTS = ("tva_cache_store", "tva_cache_load", "tva_sizeof_rows_args", "tva_tree_verify_attn_4bit", "tva_attn4_workspace_bytes",
                  "tva_attn4_plan_splits", "tva_sizeof_attn4_args", "tva_key_weights", "tva_sizeof_key_weight_args", "tva_evict_select",
                  "tva_sizeof_evict_select_args", "tva_evict_move", "tva_sizeof_evict_move_args")
+# entry points of include/tva_layer.h (bound in rotary.py and chunk.py)
+LAYER_EXPORTS = ("tva_rotary_frequencies", "tva_rotate", "tva_sizeof_rotate_args", "tva_cache_append", "tva_sizeof_append_args", "tva_chunk_attn",
+                 "tva_chunk_workspace_bytes", "tva_chunk_plan_rows", "tva_chunk_plan_splits", "tva_sizeof_chunk_args")
 # host entry points of include/tva_cast.h (bound in cast.py)
 CAST_EXPORTS = ("tva_cast_select_context", "tva_cast_select_max_valid_index", "tva_cast_layer_utility",
                 "tva_cast_layer_cost", "tva_cast_breadth_prune", "tva_cast_depth_bytes", "tva_cast_depth_init",
@@ -200,7 +205,7 @@ def _bind_native(lib) -> None:
         raise RuntimeError(f"{PYCALL_LIB_PATH} not built: run `python -c 'import __graft_entry__ as g; g.build()'`")
     from . import _pycall
     at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
-    for name in ("tva_sizeof_sample_args", "tva_sizeof_commit_args", "tva_sizeof_expand_args", *(n for n in CACHE_EXPORTS if "sizeof" in n)):
+    for name in ("tva_sizeof_sample_args", "tva_sizeof_commit_args", "tva_sizeof_expand_args", *(n for n in CACHE_EXPORTS + LAYER_EXPORTS if "sizeof" in n)):
         getattr(lib, name).restype = ctypes.c_size_t
     sizes = lib.tva_sizeof_args() + 1024 * (lib.tva_sizeof_sample_args() + 1024 * lib.tva_sizeof_commit_args())
     if _pycall.sizes != sizes or _pycall.functions != len(_NATIVE_CALLS):
@@ -211,7 +216,9 @@ def _bind_native(lib) -> None:
                         (lib.tva_sizeof_rows_args(), ("tva_cache_store", "tva_cache_load")),
                         (lib.tva_sizeof_attn4_args(), ("tva_tree_verify_attn_4bit",)),
                         (lib.tva_sizeof_key_weight_args(), ("tva_key_weights",)),
-                        (lib.tva_sizeof_evict_select_args(), ("tva_evict_select",)), (lib.tva_sizeof_evict_move_args(), ("tva_evict_move",))):
+                        (lib.tva_sizeof_evict_select_args(), ("tva_evict_select",)), (lib.tva_sizeof_evict_move_args(), ("tva_evict_move",)),
+                        (lib.tva_sizeof_rotate_args(), ("tva_rotate",)), (lib.tva_sizeof_append_args(), ("tva_cache_append",)),
+                        (lib.tva_sizeof_chunk_args(), ("tva_chunk_attn",))):
         for name in names:
             _address[name] = (at(name), size)
     _native = _pycall

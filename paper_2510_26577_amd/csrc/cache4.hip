@@ -27,7 +27,6 @@ using namespace cache_rows;
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -60,60 +59,6 @@ __device__ __forceinline__ bool find_row(const RowsParams &p, int b, int j, int 
   return true;
 }
 
-// |x| bits of the largest finite of eight bf16 numbers, and whether all are finite
-__device__ __forceinline__ uint32_t largest(const u16x8 x, bool *finite) {
-  uint32_t a = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t m = x[i] & 0x7fff;
-    a = m < 0x7f80 && m > a ? m : a;
-    all = max(all, m);
-  }
-  *finite = all < 0x7f80;
-  return a;
-}
-// Code of x / s by the borders between codes: s (at most 4 significant bits) times a border (3) is exact, and so are the comparisons.
-// NaN compares false: 0.
-__device__ __forceinline__ uint32_t code_of(float x, float s) {
-  const float a = fabsf(x);
-  const uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) + (a >= 3.5f * s) + (a > 5.f * s);
-  return c | (a == a ? (__float_as_uint(x) >> 28) & 8u : 0u);
-}
-__device__ uint32_t codes_of(const u16x8 x, float s) {
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w |= code_of(__uint_as_float((uint32_t)x[i] << 16), s) << (4 * i);
-  return w;
-}
-// The same by the conversion instructions, for finite x of at most 6 s: they divide by a power of two and round to nearest even.
-__device__ __forceinline__ uint32_t codes_k(const u16x8 x, float s) {
-  uint32_t w = 0;
-#define PAIR(i) bf16x2{__builtin_bit_cast(__bf16, (uint16_t)x[2 * i]), __builtin_bit_cast(__bf16, (uint16_t)x[2 * i + 1])}
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(0), s, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(1), s, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(2), s, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(3), s, 3);
-#undef PAIR
-  return w;
-}
-// V's scale is no power of two: the quotient comes from a reciprocal and one correction, exact where it is a border (only equality
-// with one is near enough to matter: x has 8 bits and s times a border 7).
-__device__ __forceinline__ uint32_t codes_v(const u16x8 x, float s) {
-  const float r = 1.f / s;
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float a = __uint_as_float((uint32_t)x[i] << 16), q = a * r;
-    y[i] = fmaf(fmaf(-q, s, a), r, q);
-  }
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.f, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.f, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.f, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.f, 3);
-  return w;
-}
-
 // Layers that a workgroup takes its rows of at once: what leads to a row (lengths, path, page) is read once for them.
 constexpr int kRowLayers = 4;
 
@@ -141,25 +86,12 @@ __global__ void __launch_bounds__(256) store_rows_kernel(const RowsParams p) {
   for (int l = 0; l < kRowLayers; ++l, to += p.layer_cache) {
     if (l >= here) return;
     const u16x8 k = ks[l], v = vs[l];
-    bool fk, fv;
-    uint32_t ak = largest(k, &fk), av = largest(v, &fv);
-#pragma unroll
-    for (int o = 1; o < LPR; o *= 2) {
-      if (o < 4) ak = max(ak, (uint32_t)__shfl_xor((int)ak, o));
-      av = max(av, (uint32_t)__shfl_xor((int)av, o));
-    }
-    // K: a = (1 + m/128) 2^(E-127) <= 6 * 2^e
-    const int ek = (int)(ak >> 7) - 127 - ((ak & 127) > 64 ? 1 : 2), e2 = min(max(ek, -96), 124);
-    // V: a = n/256 * 2^(E-126), the quotient by 6 rounded up to four bits
-    const int n = 128 + (int)(av & 127), ev = (int)(av >> 7) - 126;
-    const float sv = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), ev - 7) : ldexpf((float)((n + 23) / 24), ev - 6), 0x1p-96f), 0x1p124f);
-    const float sk = exponent_byte((uint32_t)(e2 + 127));
-    const bool plain = fk && fv && ek == e2 && sv > 0x1p-96f && sv < 0x1p124f;  // (else: what the instructions would do is not asked)
-    uint32_t wk = codes_k(k, sk), wv = codes_v(v, sv);
-    if (!plain) wk = codes_of(k, sk), wv = codes_of(v, sv);
+    float sv;
+    uint32_t sk;
+    const uint32_t wk = round_k<LPR>(k, &sk), wv = round_v<LPR>(v, &sv);
     ((uint32_t *)p.c.k)[to * LPR + part] = wk;
     ((uint32_t *)p.c.v)[to * LPR + part] = wv;
-    if (part % 4 == 0) ((uint8_t *)p.c.k_row_scale)[to * (D / 32) + part / 4] = (uint8_t)(e2 + 127);
+    if (part % 4 == 0) ((uint8_t *)p.c.k_row_scale)[to * (D / 32) + part / 4] = (uint8_t)sk;
     if (part == 0) ((uint16_t *)p.c.v_row_scale)[to] = (uint16_t)(__float_as_uint(sv) >> 16);
   }
 }

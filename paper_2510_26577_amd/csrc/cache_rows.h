@@ -14,6 +14,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -102,10 +103,101 @@ __device__ __forceinline__ float half_sum(float x) {
 
 __device__ __forceinline__ float exponent_byte(uint32_t x) { return __uint_as_float(x << 23); }  // 2^(x - 127), x of 1 .. 254
 
+// |x| bits of the largest finite of eight bf16 numbers, and whether all are finite
+__device__ __forceinline__ uint32_t largest(const u16x8 x, bool *finite) {
+  uint32_t a = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t m = x[i] & 0x7fff;
+    a = m < 0x7f80 && m > a ? m : a;
+    all = max(all, m);
+  }
+  *finite = all < 0x7f80;
+  return a;
+}
+// Code of x / s by the borders between codes: s (at most 4 significant bits) times a border (3) is exact, and so are the comparisons.
+// NaN compares false: 0.
+__device__ __forceinline__ uint32_t code_of(float x, float s) {
+  const float a = fabsf(x);
+  const uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) + (a >= 3.5f * s) + (a > 5.f * s);
+  return c | (a == a ? (__float_as_uint(x) >> 28) & 8u : 0u);
+}
+__device__ inline uint32_t codes_of(const u16x8 x, float s) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= code_of(__uint_as_float((uint32_t)x[i] << 16), s) << (4 * i);
+  return w;
+}
+// The same by the conversion instructions, for finite x of at most 6 s: they divide by a power of two and round to nearest even.
+__device__ __forceinline__ uint32_t codes_k(const u16x8 x, float s) {
+  uint32_t w = 0;
+#define PAIR(i) bf16x2{__builtin_bit_cast(__bf16, (uint16_t)x[2 * i]), __builtin_bit_cast(__bf16, (uint16_t)x[2 * i + 1])}
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(0), s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(1), s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(2), s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, PAIR(3), s, 3);
+#undef PAIR
+  return w;
+}
+// V's scale is no power of two: the quotient comes from a reciprocal and one correction, exact where it is a border (only equality
+// with one is near enough to matter: x has 8 bits and s times a border 7).
+__device__ __forceinline__ uint32_t codes_v(const u16x8 x, float s) {
+  const float r = 1.f / s;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = __uint_as_float((uint32_t)x[i] << 16), q = a * r;
+    y[i] = fmaf(fmaf(-q, s, a), r, q);
+  }
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.f, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.f, 3);
+  return w;
+}
+
+// Eight elements of a K row (LPR lanes have the row's, in order) -> their codes, and the scale byte of the 32 they are among.
+// a = (1 + m/128) 2^(E-127) <= 6 * 2^e
+template <int LPR>
+__device__ __forceinline__ uint32_t round_k(const u16x8 k, uint32_t *scale) {
+  bool fine;
+  uint32_t a = largest(k, &fine);
+#pragma unroll
+  for (int o = 1; o < 4; o *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+  const int e = (int)(a >> 7) - 127 - ((a & 127) > 64 ? 1 : 2), kept = min(max(e, -96), 124);
+  const float s = exponent_byte((uint32_t)(kept + 127));
+  uint32_t w = codes_k(k, s);
+  if (!(fine && e == kept)) w = codes_of(k, s);  // (what the instructions would do is not asked)
+  *scale = (uint32_t)(kept + 127);
+  return w;
+}
+// Eight elements of a V row -> their codes, and the row's scale: a = n/256 * 2^(E-126), the quotient by 6 rounded up to four bits
+template <int LPR>
+__device__ __forceinline__ uint32_t round_v(const u16x8 v, float *scale) {
+  bool fine;
+  uint32_t a = largest(v, &fine);
+#pragma unroll
+  for (int o = 1; o < LPR; o *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+  const int n = 128 + (int)(a & 127), e = (int)(a >> 7) - 126;
+  const float s = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), e - 7) : ldexpf((float)((n + 23) / 24), e - 6), 0x1p-96f), 0x1p124f);
+  uint32_t w = codes_v(v, s);
+  if (!(fine && s > 0x1p-96f && s < 0x1p124f)) w = codes_of(v, s);
+  *scale = s;
+  return w;
+}
+
 // The eight codes of a word -> bf16 values times s (a power of two, so exact).
 __device__ __forceinline__ bf16x8 widen8(uint32_t w, float s) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Four consecutive E4M3 bytes' pairs -> bf16 (exact)
+__device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 

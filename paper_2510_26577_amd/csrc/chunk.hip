@@ -1,0 +1,620 @@
+// libtva: attention of new tokens over the cache that holds them (gfx950).  Entry points and their meaning: include/tva_layer.h.
+//
+//   chunk_kernel  S^T = K Q^T and O^T = V^T P^T by 32x32x16 bf16 MFMAs, a query row per lane of a half, as in tva.hip and cache4.hip.
+//                 A workgroup has 32 * WM query rows (tokens x heads of a KV head: the heads share the keys) and walks tiles of
+//                 32 * KB * WK keys; its waves are WM row groups x WK key groups.  All waves bring a tile to LDS (through registers,
+//                 two tiles ahead; 8-bit rows are widened on the way) and read their operands there: K as rows, V by transposing
+//                 reads.  Only tiles that some row sees are walked: the first ones (of n_first), then those of the window or all.
+//   merge_kernel  partial results of row blocks whose keys were split.
+// A block's tiles are cut into equal parts, as many as the plan's length of a part asks for.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_rows.h"
+#include "sequences.h"
+#include "tva.h"
+#include "tva_cache.h"
+#include "tva_layer.h"
+
+namespace {
+
+using namespace cache_rows;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct ChunkParams {
+  const __bf16 *q;
+  const int32_t *cu_T, *L;
+  const uint64_t *mask;
+  CacheView c;
+  __bf16 *out;
+  float *lse;
+  float *part_out, *part_lse;  // [blocks, parts, Hkv, rows of a block, D], [blocks, parts, Hkv, rows]
+  int64_t q_stride;
+  int B, Hq, Hkv, G, W, blocks, max_T;
+  int parts, part_keys;  // the most parts a block's tiles are cut into, and the keys of a part that it is cut for
+  int window, n_first;   // window: 2^30 where there is none
+  float scale_log2, v_scale;
+};
+
+// A row block of one sequence: where its rows and its keys lie.
+// Blocks are numbered so that a sequence's first is known from cu_T alone: floor(cu_T[b] G / rows) + b.  A sequence of n rows has
+// ceil(n / rows) of the numbers up to the next one's first, which are at least that many.
+struct Block {
+  int b, t0, T, L;
+  int row0, rows;  // first row (token x head of the KV head) of the sequence, rows of this block
+  int low, high;   // bounds of the positions that the rows have
+  int end;         // key slots that a row may see
+  __device__ __forceinline__ static int64_t first(const ChunkParams &p, int R, int b) { return (int64_t)p.cu_T[b] * p.G / R + b; }
+  __device__ __forceinline__ Block(const ChunkParams &p, int R, int number) {
+    b = sequences::find(p.B, [&](int n) { return first(p, R, n) <= number; });
+    t0 = p.cu_T[b], T = min(p.cu_T[b + 1] - t0, p.max_T), L = max(p.L[b], 0);
+    const int64_t at = (int64_t)(number - first(p, R, b)) * R, all = (int64_t)T * p.G;
+    rows = (int)max((int64_t)0, min((int64_t)R, all - at));
+    row0 = (int)min(at, all);
+    const int64_t room = room_of(p.c, b);
+    if (p.mask) {
+      low = L - 1, high = L + T - 1;
+      end = (int)min((int64_t)L + T, room);
+    } else {
+      low = L + row0 / p.G, high = L + (row0 + max(rows, 1) - 1) / p.G;
+      end = (int)min((int64_t)high + 1, room);
+    }
+  }
+};
+// Its tiles of KT keys: `first` of them from slot 0 on, then from tile `main` on, n in all.  Those that no row sees are left out.
+struct Tiles {
+  int first, main, n;
+  __device__ __forceinline__ Tiles(const ChunkParams &p, const Block &k, int KT) {
+    const int from = max(0, k.low - p.window + 1);
+    main = min(from, max(k.end - 1, 0)) / KT;
+    first = min(main, (min(p.n_first, from) + KT - 1) / KT);
+    n = k.rows > 0 && k.end > 0 ? first + (k.end + KT - 1) / KT - main : 0;
+  }
+  __device__ __forceinline__ int at(int u) const { return u < first ? u : u - first + main; }
+  __device__ __forceinline__ int parts(const ChunkParams &p, int KT) const {
+    const int tiles = max(1, p.part_keys / KT);
+    return max(1, min(p.parts, (n + tiles - 1) / tiles));
+  }
+};
+
+__device__ __forceinline__ float half_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// whether any of eight bf16 numbers is infinite or NaN
+__device__ __forceinline__ bool not_finite(u32x4 x) {
+  bool any = false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) any |= (x[k] & 0x7f80) == 0x7f80 || (x[k] & 0x7f800000) == 0x7f800000;
+  return any;
+}
+__device__ __forceinline__ u32x4 finite_ones(u32x4 x) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if ((x[k] & 0x7f80) == 0x7f80) x[k] &= 0xffff0000u;
+    if ((x[k] & 0x7f800000) == 0x7f800000) x[k] &= 0xffffu;
+  }
+  return x;
+}
+
+template <int D, int WM, int WK, int KB, int KIND>
+struct ChunkCfg {
+  static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
+  static constexpr int R = 32 * WM, KW = 32 * KB, KT = KW * WK;
+  static constexpr int NS = D / 16, NJ = D / 32;
+  static constexpr int ROW = 2 * D, TILE = KT * ROW, STAGE = 2 * TILE;  // bytes in LDS
+  static constexpr int EPL = KIND == TVA_ROWS_BF16 || KT * D / 16 < THREADS ? 8 : 16;  // elements that a lane brings at once
+  static constexpr int LPR = D / EPL;                                                  // lanes that bring a row
+  static constexpr int NP = KT * LPR / THREADS, RPP = THREADS / LPR;   // reads per lane and tile (of K, and of V), rows of one
+  static_assert(KT * LPR % THREADS == 0, "");
+  static constexpr int TP = D + 4, PATCH = 32 * TP * 4;  // an output patch per wave, floats between its rows
+  static constexpr int EXCHANGE = 2 * WAVES * 32 * 4;
+  static constexpr int LOOP_LDS = 2 * STAGE + TVA_MAX_TREE * 4 + 2 * WAVES * 4, END_LDS = WAVES * PATCH + EXCHANGE;
+  static constexpr int LDS = LOOP_LDS > END_LDS ? LOOP_LDS : END_LDS;
+  static constexpr int PER_SIMD = LDS * 2 <= 160 * 1024 || WAVES == 8 ? 2 : 1;
+  // remainders of the softmax weights are multiplied too (their rounding to bf16 would show; the shape waits for memory)
+  static constexpr bool REST = WM == 1;
+};
+
+// Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block (the last ones, which see the
+// most keys, first).
+template <int D, int WM, int WK, int KB, int KIND, bool PAGED, bool TREE>
+__global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::PER_SIMD)) chunk_kernel(const ChunkParams p) {
+  typedef ChunkCfg<D, WM, WK, KB, KIND> C;
+  __shared__ __align__(16) unsigned char lds[C::LDS];
+  const int g = blockIdx.x, part = blockIdx.y, number = p.blocks - 1 - blockIdx.z;
+  const Block k(p, C::R, number);
+  const Tiles tiles(p, k, C::KT);
+  const int parts = tiles.parts(p, C::KT);
+  if (k.rows <= 0 || part >= parts) return;
+  const int u0 = (int)((int64_t)tiles.n * part / parts), u1 = (int)((int64_t)tiles.n * (part + 1) / parts);
+
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wm = wave % WM, wk = wave / WM;
+
+  // ---- this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written ----
+  const int row = k.row0 + min(wm * 32 + l32, k.rows - 1);
+  const int node = row / p.G, head = g * p.G + (row - node * p.G);
+  const bool idle = wm * 32 >= k.rows;
+  bf16x8 q[C::NS];
+  {
+    const __bf16 *from = p.q + (int64_t)(k.t0 + node) * p.q_stride + head * D + half * 8;
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) q[s] = *(const bf16x8 *)(from + s * 16);
+  }
+  int P = k.L + node;
+  uint64_t anc0 = 0, anc1 = 0;
+  if constexpr (TREE) {
+    int *depth = (int *)(lds + 2 * C::STAGE);
+    for (int i = tid; i < k.T; i += C::THREADS) {
+      const uint64_t *words = p.mask + (int64_t)(k.t0 + i) * p.W;
+      depth[i] = (int)__popcll(words[0]) + (p.W > 1 ? (int)__popcll(words[1]) : 0) - 1;
+    }
+    __syncthreads();
+    const uint64_t *words = p.mask + (int64_t)(k.t0 + node) * p.W;
+    anc0 = words[0], anc1 = p.W > 1 ? words[1] : 0;
+    P = k.L + (int)__popcll(anc0) + (int)__popcll(anc1) - 1;
+    if (k.T < 64) anc0 &= (1ull << k.T) - 1, anc1 = 0;
+    else if (k.T < 128) anc1 &= (1ull << (k.T - 64)) - 1;
+    for (uint64_t left = anc0; left; left &= left - 1) {  // what the window leaves of them
+      const int j = __builtin_ctzll(left), at = k.L + depth[j];
+      if (at <= P - p.window && at >= p.n_first) anc0 &= ~(1ull << j);
+    }
+    for (uint64_t left = anc1; left; left &= left - 1) {
+      const int j = __builtin_ctzll(left), at = k.L + depth[64 + j];
+      if (at <= P - p.window && at >= p.n_first) anc1 &= ~(1ull << j);
+    }
+  }
+  const int behind = P - p.window;  // positions up to it are out of the window
+  // Which of the 32 key slots from t on this lane's row sees, a bit each.  (Bits, not comparisons: those of a whole tile at once are more
+  // than there are scalar registers.)
+  auto below = [](int n) __attribute__((always_inline)) -> uint32_t { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+  auto sees = [&](int t) __attribute__((always_inline)) -> uint32_t {
+    const uint32_t near = ~below(behind + 1 - t) | below(p.n_first - t);
+    if constexpr (TREE) {
+      const int j = t - k.L;  // the first one's number among the new tokens
+      uint32_t bits = near & below(-j);
+      if (j > -32) bits |= (uint32_t)(j < 0 ? anc0 << -j : j < 64 ? anc0 >> j : j < 128 ? anc1 >> (j - 64) : 0);
+      if (j > 32 && j < 64) bits |= (uint32_t)(anc1 << (64 - j));
+      return bits & below(k.end - t);
+    } else {
+      return near & below(min(P + 1, k.end) - t);
+    }
+  };
+  // bounds over the wave's rows, the same for all its lanes
+  int low = k.low, high = k.high;
+  if constexpr (!TREE) {
+    low = k.L + (k.row0 + min(wm * 32, k.rows - 1)) / p.G, high = k.L + (k.row0 + min(wm * 32 + 31, k.rows - 1)) / p.G;
+    low = __builtin_amdgcn_readfirstlane(low), high = __builtin_amdgcn_readfirstlane(high);
+  }
+  // whether all rows with positions low .. high see the n slots from t on
+  auto all_seen = [&](int t, int n, int low, int high) __attribute__((always_inline)) -> bool {
+    return t + n <= k.end && t + n - 1 <= (TREE ? k.L - 1 : low) && (t > high - p.window || t + n <= p.n_first);
+  };
+
+  // ---- tiles: global memory -> registers -> LDS ----
+  const Finder<PAGED> find(p.c, k.b, g);
+  const int piece = tid % C::LPR, prow = tid / C::LPR;
+  u32x4 kx[C::NP], vx[C::NP];
+  int entry[C::NP];
+  auto slot = [&](int u, int i) __attribute__((always_inline)) { return min(tiles.at(min(u, u1 - 1)) * C::KT + i * C::RPP + prow, k.end - 1); };
+  auto look = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, slot(u, i));
+  };
+  auto fetch = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::NP; ++i) {
+      const int64_t at = find.at(p.c, slot(u, i), entry[i]);
+      if constexpr (KIND == TVA_ROWS_BF16) {
+        kx[i] = *(const u32x4 *)(p.c.k + (at + piece * 8) * 2);
+        vx[i] = *(const u32x4 *)(p.c.v + (at + piece * 8) * 2);
+      } else if constexpr (C::EPL == 16) {
+        kx[i] = *(const u32x4 *)(p.c.k + at + piece * 16);
+        vx[i] = *(const u32x4 *)(p.c.v + at + piece * 16);
+      } else {
+        const u32x2 a = *(const u32x2 *)(p.c.k + at + piece * 8), b = *(const u32x2 *)(p.c.v + at + piece * 8);
+        kx[i] = u32x4{a[0], a[1], 0, 0}, vx[i] = u32x4{b[0], b[1], 0, 0};
+      }
+    }
+  };
+  // Where 16-byte piece c of row r lies in its row, so that the lanes of a read are in different banks: 16 rows of K at one piece each; of V
+  // four consecutive rows, 64 bytes of each.
+  auto k_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); };
+  auto v_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); };
+  int *odd_at = (int *)(lds + 2 * C::STAGE + TVA_MAX_TREE * 4);  // [2][WAVES]: a value of the tile is not finite
+  auto stash = [&](int u) __attribute__((always_inline)) {
+    unsigned char *to = lds + (u & 1) * C::STAGE;
+    const int first = tiles.at(u) * C::KT;
+    const bool careful = C::REST || !all_seen(first, C::KT, k.low, k.high);  // (an infinite value times a remainder of 0 or below is no infinity)
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < C::NP; ++i) {
+      const int r = i * C::RPP + prow;
+      if constexpr (KIND == TVA_ROWS_BF16) {
+        *(u32x4 *)(to + r * C::ROW + k_piece(r, piece) * 16) = kx[i];
+        if (careful && not_finite(vx[i])) odd = true, vx[i] = finite_ones(vx[i]);
+        *(u32x4 *)(to + C::TILE + r * C::ROW + v_piece(r, piece) * 16) = vx[i];
+      } else {
+#pragma unroll
+        for (int h = 0; h < C::EPL / 8; ++h) {
+          *(bf16x8 *)(to + r * C::ROW + k_piece(r, C::EPL / 8 * piece + h) * 16) = widen8_e4m3(u32x2{kx[i][2 * h], kx[i][2 * h + 1]});
+          u32x4 v = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i][2 * h], vx[i][2 * h + 1]}));
+          if (careful && not_finite(v)) odd = true, v = finite_ones(v);
+          *(u32x4 *)(to + C::TILE + r * C::ROW + v_piece(r, C::EPL / 8 * piece + h) * 16) = v;
+        }
+      }
+    }
+    if (careful) {
+      const bool any = __any(odd);
+      if (lane == 0) odd_at[(u & 1) * C::WAVES + wave] = any;
+    }
+  };
+
+  f32x16 acc[C::NJ];
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j) acc[j] = f32x16{};
+  float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
+  f32x16 s[KB];
+
+  auto compute = [&](int u) __attribute__((always_inline)) {
+    const unsigned char *kt = lds + (u & 1) * C::STAGE + wk * C::KW * C::ROW, *vt = kt + C::TILE;
+    const int first = tiles.at(u) * C::KT, t0 = first + wk * C::KW;
+    // (a tile with a value that is not finite: all waves of the workgroup take the long way)
+    bool odd = false;
+    if (C::REST || !all_seen(first, C::KT, k.low, k.high)) {
+#pragma unroll
+      for (int w = 0; w < C::WAVES; ++w) odd |= odd_at[(u & 1) * C::WAVES + w] != 0;
+      odd = __builtin_amdgcn_readfirstlane(odd);
+    }
+    const bool masked = !all_seen(t0, C::KW, low, high);
+    if (masked) {
+      const bool none = t0 >= k.end || (!TREE && t0 > high) || (t0 + C::KW - 1 <= low - p.window && t0 >= p.n_first && (!TREE || t0 + C::KW <= k.L));
+      if (none) return;
+    }
+    // ---- S^T = K Q^T
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+#pragma unroll
+    for (int st = 0; st < C::NS; ++st)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const bf16x8 x = *(const bf16x8 *)(kt + (kb * 32 + l32) * C::ROW + k_piece(l32, st * 2 + half) * 16);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[st], s[kb], 0, 0, 0);
+      }
+    if (masked) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const uint32_t bits = sees(t0 + kb * 32) >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[kb][i] = -INFINITY;
+      }
+    }
+    // ---- scores -> weights in place; O and l move to a new reference where a row's largest score exceeds it by more than 2^8
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+    top = half_max(top) * p.scale_log2;
+    if (__any(top > m + 8.f)) {
+      const float to = fmaxf(m, top);
+      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to, l *= f;
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[j][i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, -ref));
+        l += s[kb][i];
+      }
+    // ---- O^T += V^T P^T: 16 lanes turn over 4 rows x 16 elements: this lane's row (of keys 8 h + 4 half + 0..3) and 8-byte piece of it
+    const int i16 = lane & 15, sub = (lane >> 4) & 1;
+    if (odd) {  // what is not finite was taken out of the tile: rows that see it get it added
+      for (int x = 0; x < C::KW; ++x) {
+        const int t = t0 + x;
+        if (t >= k.end) break;
+        const bool here = sees(t) & 1;
+        const int64_t at = find.at(p.c, t, find.entry(p.c, t));
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int d = 32 * j + 8 * (i / 4) + 4 * half + i % 4;
+            float v;
+            if constexpr (KIND == TVA_ROWS_BF16) v = (float)((const __bf16 *)p.c.v)[at + d];
+            else v = (((const uint8_t *)p.c.v)[at + d] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+            if (here && !__builtin_isfinite(v)) acc[j][i] += v;
+          }
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        bf16x8 w, rest;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          w[i] = (__bf16)s[kb][a * 8 + i];
+          if constexpr (C::REST) rest[i] = (__bf16)(s[kb][a * 8 + i] - (float)w[i]);
+        }
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j) {
+          s16x4 c[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = 32 * kb + 16 * a + 8 * h + 4 * half + (i16 >> 2);
+            c[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)(vt + r * C::ROW + v_piece(i16 >> 2, j * 4 + sub * 2) * 16 + (i16 & 3) * 8));
+          }
+          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
+          if constexpr (C::REST) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest, acc[j], 0, 0, 0);
+        }
+      }
+  };
+
+  if (u0 < u1) {
+    look(u0);
+    fetch(u0);
+    look(u0 + 1);
+    stash(u0);
+    fetch(u0 + 1);
+    look(u0 + 2);
+    __syncthreads();
+    for (int u = u0; u < u1; ++u) {
+      if (u + 1 < u1) {
+        stash(u + 1);
+        fetch(u + 2);
+        look(u + 3);
+      }
+      if (!idle) compute(u);
+      __syncthreads();
+    }
+  }
+
+  // ---- the key groups' results joined, and O^T turned over to rows ----
+  l = half_sum(l);
+  __syncthreads();
+  float *patch = (float *)lds, *maxima = (float *)(lds + C::WAVES * C::PATCH), *sums = maxima + C::WAVES * 32;
+  if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int x = 0; x < WK; ++x) top = fmaxf(top, maxima[(x * WM + wm) * 32 + l32]);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = acc[j][i * 4 + e] * f;
+      *(f32x4 *)(patch + wave * (32 * C::TP) + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
+    }
+  __syncthreads();
+  const int64_t slot0 = (((int64_t)number * p.parts + part) * p.Hkv + g) * C::R;
+  for (int x = tid; x < C::R * (D / 4); x += C::THREADS) {
+    const int r = x / (D / 4), d = (x - r * (D / 4)) * 4, w = r >> 5, rr = r & 31;
+    if (r >= k.rows) break;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float top_r = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int y = 0; y < WK; ++y) top_r = fmaxf(top_r, maxima[(y * WM + w) * 32 + rr]);
+#pragma unroll
+    for (int y = 0; y < WK; ++y) {
+      const int at = y * WM + w;
+      o += *(const f32x4 *)(patch + at * (32 * C::TP) + rr * C::TP + d);
+      const float my = maxima[at * 32 + rr];
+      sum += my == -INFINITY ? sums[at * 32 + rr] : sums[at * 32 + rr] * __builtin_amdgcn_exp2f(my - top_r);  // (0, or NaN)
+    }
+    o *= sum == 0.f ? 0.f : p.v_scale / sum;  // (NaN stays NaN)
+    const float lse = sum == 0.f ? -INFINITY : (top_r + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
+    if (parts == 1) {
+      const int rnode = (k.row0 + r) / p.G, rhead = g * p.G + (k.row0 + r - rnode * p.G);
+      const int64_t at = (int64_t)(k.t0 + rnode) * p.Hq + rhead;
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (__bf16)o[e];
+      *(bf16x4 *)(p.out + at * D + d) = y;
+      if (d == 0 && p.lse) p.lse[at] = lse;
+    } else {
+      *(f32x4 *)(p.part_out + (slot0 + r) * D + d) = o;
+      if (d == 0) p.part_lse[slot0 + r] = lse;
+    }
+  }
+}
+
+// lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s, D/4 lanes per row, eight parts in flight.
+// Grid: KV head, rows of a block (1024 / D at a time), block.
+template <int D, int R>
+__global__ void __launch_bounds__(256) merge_kernel(const ChunkParams p, int KT) {
+  constexpr int LPR = D / 4, U = 8, ROWS = 256 / LPR;
+  const int g = blockIdx.x, r = blockIdx.y * ROWS + threadIdx.x / LPR, number = blockIdx.z;
+  const Block k(p, R, number);
+  const int S = Tiles(p, k, KT).parts(p, KT);
+  if (S == 1 || r >= k.rows) return;
+  const int64_t stride = (int64_t)p.Hkv * R, slot0 = ((int64_t)number * p.parts * p.Hkv + g) * R + r;
+  const int d = (threadIdx.x % LPR) * 4;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, sum = 0.f;
+  for (int s0 = 0; s0 < S; s0 += U) {
+    float ls[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = slot0 + min(s0 + u, S - 1) * stride;
+      ls[u] = p.part_lse[at];
+      x[u] = *(const f32x4 *)(p.part_out + at * D + d);
+    }
+    float here = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) here = fmaxf(here, ls[u]);
+    const float f = here == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - here) * kLog2e);
+    o *= f, sum *= f, top = here;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + u >= S || ls[u] == -INFINITY) continue;
+      const float w = __builtin_amdgcn_exp2f((ls[u] - (top == -INFINITY ? 0.f : top)) * kLog2e);
+      sum += w;
+      o += x[u] * w;
+    }
+  }
+  o *= sum == 0.f ? 0.f : 1.f / sum;
+  bf16x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (__bf16)o[e];
+  const int node = (k.row0 + r) / p.G, head = g * p.G + (k.row0 + r - node * p.G);
+  const int64_t at = (int64_t)(k.t0 + node) * p.Hq + head;
+  *(bf16x4 *)(p.out + at * D + d) = y;
+  if (d == 0 && p.lse) p.lse[at] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+}
+
+struct ChunkPlan {
+  int rows, KT;    // of a workgroup, keys of its tiles
+  int blocks;
+  int parts, part_keys;
+};
+void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
+  const int G = a->Hq / a->Hkv;
+  const int64_t rows = (int64_t)a->max_T * G;
+  pl->rows = a->plan_rows ? a->plan_rows : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  pl->KT = pl->rows == 32 ? 128 : 64;
+  const int64_t blocks = (int64_t)a->sum_T * G / pl->rows + a->B;
+  pl->blocks = (int)std::min<int64_t>(blocks, 0x7fffffff);
+  // keys that a row block may see
+  const int64_t seen = a->window ? std::min<int64_t>((int64_t)a->max_L + a->max_T, (int64_t)a->window + a->n_first + pl->rows / G + 2 * pl->KT) : (int64_t)a->max_L + a->max_T;
+  const int64_t tiles = std::max<int64_t>(1, (seen + pl->KT - 1) / pl->KT);
+  const int slots = pl->rows == 32 || pl->rows == 256 ? 256 : 512;
+  // row blocks that have rows: a sequence of max_T tokens has this many
+  const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(blocks, (int64_t)a->B * ((rows + pl->rows - 1) / pl->rows))) * a->Hkv;
+  int64_t parts = a->num_splits;
+  if (parts == 0) parts = busy >= 2 * slots ? 1 : std::max<int64_t>(1, slots / busy);
+  parts = std::max<int64_t>(1, std::min<int64_t>(parts, tiles));
+  pl->part_keys = (int)((tiles + parts - 1) / parts) * pl->KT;
+  pl->parts = (int)parts;
+}
+
+int check_chunk(const tva_chunk_args *a, bool shapes_only) {
+  if (!a || a->B <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv) return TVA_INVALID_ARG;
+  if (a->sum_T < 0 || a->max_T < 0 || a->max_L < 0 || a->num_splits < 0 || a->window < 0 || a->n_first < 0) return TVA_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
+  if (a->plan_rows != 0 && a->plan_rows != 32 && a->plan_rows != 64 && a->plan_rows != 128 && a->plan_rows != 256) return TVA_INVALID_ARG;
+  if (a->max_L > 1 << 29 || a->max_T > 1 << 28 || (int64_t)a->max_T * (a->Hq / a->Hkv) > 1 << 30) return TVA_UNSUPPORTED;  // (positions below 2^30)
+  if (a->anc_mask && (a->max_T > TVA_MAX_TREE || a->mask_words < 1 || a->mask_words > 2 || a->mask_words * 64 < a->max_T)) return TVA_UNSUPPORTED;
+  if (shapes_only) return TVA_OK;
+  if (!(a->scale > 0.f)) return TVA_INVALID_ARG;
+  if (a->cache.kind < TVA_ROWS_BF16 || a->cache.kind > TVA_ROWS_E2M1) return TVA_INVALID_ARG;
+  if (a->cache.kind == TVA_ROWS_E2M1) return TVA_UNSUPPORTED;
+  if (a->q_stride && (a->q_stride % 8 || a->q_stride < (int64_t)a->Hq * a->D)) return TVA_INVALID_ARG;
+  if (a->sum_T == 0) return TVA_OK;
+  if (!a->cu_T || !a->L || !a->q || !a->out) return TVA_INVALID_ARG;
+  if (((uintptr_t)a->q | (uintptr_t)a->out) & 15) return TVA_INVALID_ARG;
+  return TVA_OK;
+}
+
+size_t chunk_bytes(const tva_chunk_args *a, const ChunkPlan &pl) {
+  return pl.parts == 1 ? 0 : (size_t)pl.blocks * pl.parts * a->Hkv * pl.rows * (a->D + 1) * 4;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tva_chunk_workspace_bytes(const tva_chunk_args *a) {
+  ChunkPlan pl;
+  if (check_chunk(a, true) != TVA_OK) return (size_t)-1;
+  plan_chunk(a, &pl);
+  return chunk_bytes(a, pl);
+}
+
+int32_t tva_chunk_plan_rows(const tva_chunk_args *a) {
+  ChunkPlan pl;
+  if (check_chunk(a, true) != TVA_OK) return -1;
+  plan_chunk(a, &pl);
+  return pl.rows;
+}
+
+int32_t tva_chunk_plan_splits(const tva_chunk_args *a) {
+  ChunkPlan pl;
+  if (check_chunk(a, true) != TVA_OK) return -1;
+  plan_chunk(a, &pl);
+  return pl.parts;
+}
+
+int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
+  int rc = check_chunk(a, false);
+  if (rc != TVA_OK) return rc;
+  ChunkParams p{};
+  rc = view_of(a->cache, a->Hkv, a->D, true, &p.c);
+  if (rc != TVA_OK) return rc;
+  if (a->sum_T == 0 || a->max_T == 0) return TVA_OK;
+  ChunkPlan pl;
+  plan_chunk(a, &pl);
+  const size_t need = chunk_bytes(a, pl);
+  if (need && (!a->workspace || ((uintptr_t)a->workspace & 15))) return TVA_INVALID_ARG;
+  if (a->workspace_bytes < need) return TVA_WORKSPACE_TOO_SMALL;
+  if (pl.blocks > 65535 || pl.parts > 65535) return TVA_UNSUPPORTED;
+  const bool eight = a->cache.kind == TVA_ROWS_E4M3;
+  const float k_scale = !eight || a->cache.k_scale == 0.f ? 1.f : a->cache.k_scale;
+  p.q = (const __bf16 *)a->q, p.cu_T = a->cu_T, p.L = a->L, p.mask = a->anc_mask;
+  p.out = (__bf16 *)a->out, p.lse = a->lse;
+  p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (need ? need / 4 / (a->D + 1) * a->D : 0);
+  p.q_stride = a->q_stride ? a->q_stride : (int64_t)a->Hq * a->D;
+  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.blocks = pl.blocks, p.max_T = a->max_T;
+  p.parts = pl.parts, p.part_keys = pl.part_keys;
+  p.window = a->window ? std::min(a->window, 1 << 30) : 1 << 30, p.n_first = a->window ? a->n_first : 0;
+  p.scale_log2 = a->scale * kLog2e * k_scale, p.v_scale = !eight || a->cache.v_scale == 0.f ? 1.f : a->cache.v_scale;
+  const dim3 grid(a->Hkv, pl.parts, pl.blocks);
+  const hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  auto launch = [&](auto d, auto wm, auto wk, auto kb) {
+    constexpr int D = decltype(d)::value, WM = decltype(wm)::value, WK = decltype(wk)::value, KB = decltype(kb)::value, THREADS = 64 * WM * WK;
+    auto form = [&](auto kind) {
+      constexpr int KIND = decltype(kind)::value;
+      static_assert(32 * KB * WK == (WM == 1 ? 128 : 64), "plan_chunk");
+      if (a->cache.page_table) {
+        if (a->anc_mask) hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, true, true>), grid, dim3(THREADS), 0, st, p);
+        else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, true, false>), grid, dim3(THREADS), 0, st, p);
+      } else {
+        if (a->anc_mask) hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, false, true>), grid, dim3(THREADS), 0, st, p);
+        else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, false, false>), grid, dim3(THREADS), 0, st, p);
+      }
+    };
+    if (eight) form(std::integral_constant<int, TVA_ROWS_E4M3>{});
+    else form(std::integral_constant<int, TVA_ROWS_BF16>{});
+    if (pl.parts > 1 && hipPeekAtLastError() == hipSuccess)
+      hipLaunchKernelGGL((merge_kernel<D, 32 * WM>), dim3(a->Hkv, 32 * WM / (1024 / D), pl.blocks), dim3(256), 0, st, p, pl.KT);
+  };
+  typedef std::integral_constant<int, 1> one;
+  typedef std::integral_constant<int, 2> two;
+  typedef std::integral_constant<int, 4> four;
+  typedef std::integral_constant<int, 8> many;
+  auto shapes = [&](auto d) {
+    if (pl.rows == 32) launch(d, one{}, four{}, one{});
+    else if (pl.rows == 64) launch(d, two{}, two{}, one{});
+    else if (pl.rows == 128) launch(d, four{}, one{}, two{});
+    else launch(d, many{}, one{}, two{});
+  };
+  if (a->D == 128) shapes(std::integral_constant<int, 128>{});
+  else shapes(std::integral_constant<int, 64>{});
+  return hipPeekAtLastError() == hipSuccess ? TVA_OK : TVA_HIP_ERROR;
+}
+
+size_t tva_sizeof_chunk_args(void) { return sizeof(tva_chunk_args); }
+
+}  // extern "C"

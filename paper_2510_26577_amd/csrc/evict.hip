@@ -38,13 +38,6 @@ struct WeighParams {
   float scale_log2;
 };
 
-// Four consecutive E4M3 bytes' pairs -> bf16 (exact)
-__device__ __forceinline__ bf16x8 widen8_e4m3(u32x2 w) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
 constexpr int kWeighWaves = 4;
 
 // What a lane reads of a K row, as it lies in the cache: elements 16 s + 8 half of step s (bf16), or half of the row per lane half.

@@ -2709,7 +2709,7 @@ int static_scratch(void **out) {
 
 extern "C" {
 
-int tva_version(void) { return 7; }
+int tva_version(void) { return 8; }
 
 int tva_timeline_read(uint64_t *dst, int32_t n_workgroups) {
 #ifdef TVA_TIMELINE
