@@ -120,7 +120,7 @@ typedef struct tva_chunk_args {
   const void *q;                /* device bf16, head h of row r at r * q_stride + h * D */
   int64_t q_stride;             /* elements, multiple of 8; 0 = packed */
   const uint64_t *anc_mask;     /* device [sum_T, mask_words] or NULL */
-  tva_cache cache;              /* kind BF16 or E4M3 */
+  tva_cache cache;              /* kind BF16 or E4M3; stride_tok below 2^25 */
   void *out;                    /* device bf16 [sum_T, Hq, D] */
   float *lse;                   /* device fp32 [sum_T, Hq] or NULL */
   void *workspace;              /* device, 16-byte aligned */

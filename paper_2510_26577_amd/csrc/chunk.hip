@@ -43,6 +43,9 @@ struct ChunkParams {
   float scale_log2, v_scale;
 };
 
+// (The compiler takes what a wave finds by asking its lanes for a value per lane: said once, here.)
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // A row block of one sequence: where its rows and its keys lie.
 // Blocks are numbered so that a sequence's first is known from cu_T alone: floor(cu_T[b] G / rows) + b.  A sequence of n rows has
 // ceil(n / rows) of the numbers up to the next one's first, which are at least that many.
@@ -51,13 +54,13 @@ struct Block {
   int row0, rows;  // first row (token x head of the KV head) of the sequence, rows of this block
   int low, high;   // bounds of the positions that the rows have
   int end;         // key slots that a row may see
-  __device__ __forceinline__ static int64_t first(const ChunkParams &p, int R, int b) { return (int64_t)p.cu_T[b] * p.G / R + b; }
   __device__ __forceinline__ Block(const ChunkParams &p, int R, int number) {
-    b = sequences::find(p.B, [&](int n) { return first(p, R, n) <= number; });
-    t0 = p.cu_T[b], T = min(p.cu_T[b + 1] - t0, p.max_T), L = max(p.L[b], 0);
-    const int64_t at = (int64_t)(number - first(p, R, b)) * R, all = (int64_t)T * p.G;
-    rows = (int)max((int64_t)0, min((int64_t)R, all - at));
-    row0 = (int)min(at, all);
+    auto first = [&](int n, int row) __attribute__((always_inline)) { return (int64_t)row * p.G / R + n; };
+    const sequences::Place place = sequences::find(p.cu_T, p.L, p.B, number, first);
+    b = same(place.b), t0 = same(place.t0), T = same(min(place.t1 - place.t0, p.max_T)), L = same(max(place.L, 0));
+    const int64_t at = (int64_t)(number - first(b, t0)) * R, all = (int64_t)T * p.G;
+    rows = same((int)max((int64_t)0, min((int64_t)R, all - at)));
+    row0 = same((int)min(at, all));
     const int64_t room = room_of(p.c, b);
     if (p.mask) {
       low = L - 1, high = L + T - 1;
@@ -66,6 +69,7 @@ struct Block {
       low = L + row0 / p.G, high = L + (row0 + max(rows, 1) - 1) / p.G;
       end = (int)min((int64_t)high + 1, room);
     }
+    low = same(low), high = same(high), end = same(end);
   }
 };
 // Its tiles of KT keys: `first` of them from slot 0 on, then from tile `main` on, n in all.  Those that no row sees are left out.
@@ -75,12 +79,13 @@ struct Tiles {
     const int from = max(0, k.low - p.window + 1);
     main = min(from, max(k.end - 1, 0)) / KT;
     first = min(main, (min(p.n_first, from) + KT - 1) / KT);
-    n = k.rows > 0 && k.end > 0 ? first + (k.end + KT - 1) / KT - main : 0;
+    n = same(k.rows > 0 && k.end > 0 ? first + (k.end + KT - 1) / KT - main : 0);
+    first = same(first), main = same(main);
   }
   __device__ __forceinline__ int at(int u) const { return u < first ? u : u - first + main; }
   __device__ __forceinline__ int parts(const ChunkParams &p, int KT) const {
     const int tiles = max(1, p.part_keys / KT);
-    return max(1, min(p.parts, (n + tiles - 1) / tiles));
+    return same(max(1, min(p.parts, (n + tiles - 1) / tiles)));
   }
 };
 
@@ -107,26 +112,34 @@ __device__ __forceinline__ u32x4 finite_ones(u32x4 x) {
 template <int D, int WM, int WK, int KB, int KIND>
 struct ChunkCfg {
   static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
-  static constexpr int R = 32 * WM, KW = 32 * KB, KT = KW * WK;
+  // 32-row workgroups: a wave brings tiles of its own and waits for no other; else the workgroup's waves bring one together
+  static constexpr bool OWN = WM == 1;
+  static constexpr int R = 32 * WM, KW = 32 * KB, KT = OWN ? KW : KW * WK;  // rows; keys of a tile that a wave multiplies, and of a tile
+  static constexpr int STEP = OWN ? WK : 1;                                // tiles from one of a wave's to its next
   static constexpr int NS = D / 16, NJ = D / 32;
   static constexpr int ROW = 2 * D, TILE = KT * ROW, STAGE = 2 * TILE;  // bytes in LDS
-  static constexpr int EPL = KIND == TVA_ROWS_BF16 || KT * D / 16 < THREADS ? 8 : 16;  // elements that a lane brings at once
-  static constexpr int LPR = D / EPL;                                                  // lanes that bring a row
-  static constexpr int NP = KT * LPR / THREADS, RPP = THREADS / LPR;   // reads per lane and tile (of K, and of V), rows of one
-  static_assert(KT * LPR % THREADS == 0, "");
+  static constexpr int STAGES = OWN ? WK : 2;
+  static constexpr int TOGETHER = OWN ? 1 : WAVES;                        // waves that bring a tile
+  static constexpr int EPL = KIND == TVA_ROWS_BF16 || KT * D / 16 < 64 * TOGETHER ? 8 : 16;  // elements that a lane brings at once
+  static constexpr int LPR = D / EPL, RPW = 64 / LPR;                     // lanes that bring a row, rows that a wave brings at once
+  static constexpr int NP = KT / (RPW * TOGETHER);                        // reads per lane and tile (of K, and of V)
+  static_assert(KT % (RPW * TOGETHER) == 0, "");
   static constexpr int TP = D + 4, PATCH = 32 * TP * 4;  // an output patch per wave, floats between its rows
   static constexpr int EXCHANGE = 2 * WAVES * 32 * 4;
-  static constexpr int LOOP_LDS = 2 * STAGE + TVA_MAX_TREE * 4 + 2 * WAVES * 4, END_LDS = WAVES * PATCH + EXCHANGE;
+  static constexpr int DEPTH = STAGES * STAGE, ODD = DEPTH + TVA_MAX_TREE * 4;  // LDS: tiles, depths of a tree's nodes, marks of tiles
+  static constexpr int LOOP_LDS = ODD + 2 * WAVES * 4, END_LDS = WAVES * PATCH + EXCHANGE;
   static constexpr int LDS = LOOP_LDS > END_LDS ? LOOP_LDS : END_LDS;
-  static constexpr int PER_SIMD = LDS * 2 <= 160 * 1024 || WAVES == 8 ? 2 : 1;
   // remainders of the softmax weights are multiplied too (their rounding to bf16 would show; the shape waits for memory)
   static constexpr bool REST = WM == 1;
 };
 
 // Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block (the last ones, which see the
 // most keys, first).
-template <int D, int WM, int WK, int KB, int KIND, bool PAGED, bool TREE>
-__global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::PER_SIMD)) chunk_kernel(const ChunkParams p) {
+// PLACES: how a tile's rows are found.  kDense and kPages: the rows that a wave brings at once lie in a sequence, or a page, one after the
+// other: scalar addresses and a lane's offset; kRows: each lane looks for its own (pages that such rows may straddle).
+enum { kDense, kPages, kRows };
+template <int D, int WM, int WK, int KB, int KIND, int PLACES, bool TREE>
+__global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams p) {
   typedef ChunkCfg<D, WM, WK, KB, KIND> C;
   __shared__ __align__(16) unsigned char lds[C::LDS];
   const int g = blockIdx.x, part = blockIdx.y, number = p.blocks - 1 - blockIdx.z;
@@ -134,7 +147,7 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
   const Tiles tiles(p, k, C::KT);
   const int parts = tiles.parts(p, C::KT);
   if (k.rows <= 0 || part >= parts) return;
-  const int u0 = (int)((int64_t)tiles.n * part / parts), u1 = (int)((int64_t)tiles.n * (part + 1) / parts);
+  const int u0 = same((int)((int64_t)tiles.n * part / parts)), u1 = same((int)((int64_t)tiles.n * (part + 1) / parts));
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wm = wave % WM, wk = wave / WM;
@@ -152,7 +165,7 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
   int P = k.L + node;
   uint64_t anc0 = 0, anc1 = 0;
   if constexpr (TREE) {
-    int *depth = (int *)(lds + 2 * C::STAGE);
+    int *depth = (int *)(lds + C::DEPTH);
     for (int i = tid; i < k.T; i += C::THREADS) {
       const uint64_t *words = p.mask + (int64_t)(k.t0 + i) * p.W;
       depth[i] = (int)__popcll(words[0]) + (p.W > 1 ? (int)__popcll(words[1]) : 0) - 1;
@@ -200,27 +213,44 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
   };
 
   // ---- tiles: global memory -> registers -> LDS ----
-  const Finder<PAGED> find(p.c, k.b, g);
-  const int piece = tid % C::LPR, prow = tid / C::LPR;
+  const Finder<PLACES != kDense> find(p.c, k.b, g);
+  const int piece = lane % C::LPR, lrow = lane / C::LPR, bring = C::OWN ? 0 : wave;
+  const int last = k.end - 1, last_group = last - last % C::RPW;  // the last slot, and the first of the group that it is in
+  constexpr int BYTES = KIND == TVA_ROWS_BF16 ? 2 : 1;            // of an element
   u32x4 kx[C::NP], vx[C::NP];
-  int entry[C::NP];
-  auto slot = [&](int u, int i) __attribute__((always_inline)) { return min(tiles.at(min(u, u1 - 1)) * C::KT + i * C::RPP + prow, k.end - 1); };
+  int entry[PLACES == kRows ? C::NP : 1];  // kRows: the page of this lane's row of each read; kPages: lane i has that of read i
+  // (a tile past the last one: the last again.  A branch would leave the waits without a count to go by)
+  auto first_slot = [&](int u) __attribute__((always_inline)) { return tiles.at(min(u, u1 - 1)) * C::KT; };
   auto look = [&](int u) __attribute__((always_inline)) {
+    const int t = first_slot(u);
+    if constexpr (PLACES == kRows) {
 #pragma unroll
-    for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, slot(u, i));
+      for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last));
+    } else if constexpr (PLACES == kPages) {
+      entry[0] = find.entry(p.c, min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group));
+    }
   };
   auto fetch = [&](int u) __attribute__((always_inline)) {
+    const int t = first_slot(u);
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
-      const int64_t at = find.at(p.c, slot(u, i), entry[i]);
-      if constexpr (KIND == TVA_ROWS_BF16) {
-        kx[i] = *(const u32x4 *)(p.c.k + (at + piece * 8) * 2);
-        vx[i] = *(const u32x4 *)(p.c.v + (at + piece * 8) * 2);
-      } else if constexpr (C::EPL == 16) {
-        kx[i] = *(const u32x4 *)(p.c.k + at + piece * 16);
-        vx[i] = *(const u32x4 *)(p.c.v + at + piece * 16);
+      const char *from_k, *from_v;
+      if constexpr (PLACES == kRows) {
+        const int row = min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last);
+        const int64_t at = (find.at(p.c, row, entry[i]) + piece * C::EPL) * BYTES;
+        from_k = p.c.k + at, from_v = p.c.v + at;
       } else {
-        const u32x2 a = *(const u32x2 *)(p.c.k + at + piece * 8), b = *(const u32x2 *)(p.c.v + at + piece * 8);
+        const int row = min(t + (i * C::TOGETHER + bring) * C::RPW, last_group);
+        int64_t at;
+        if constexpr (PLACES == kPages) at = find.at(p.c, row, __builtin_amdgcn_readlane(entry[0], i)) * BYTES;
+        else at = find.at(p.c, row, 0) * BYTES;
+        const uint32_t off = (uint32_t)min(lrow, last - row) * (uint32_t)(p.c.stride_tok * BYTES) + (uint32_t)(piece * C::EPL * BYTES);
+        from_k = p.c.k + at + off, from_v = p.c.v + at + off;
+      }
+      if constexpr (C::EPL * BYTES == 16) {
+        kx[i] = *(const u32x4 *)from_k, vx[i] = *(const u32x4 *)from_v;
+      } else {
+        const u32x2 a = *(const u32x2 *)from_k, b = *(const u32x2 *)from_v;
         kx[i] = u32x4{a[0], a[1], 0, 0}, vx[i] = u32x4{b[0], b[1], 0, 0};
       }
     }
@@ -229,15 +259,17 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
   // four consecutive rows, 64 bytes of each.
   auto k_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); };
   auto v_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); };
-  int *odd_at = (int *)(lds + 2 * C::STAGE + TVA_MAX_TREE * 4);  // [2][WAVES]: a value of the tile is not finite
-  auto stash = [&](int u) __attribute__((always_inline)) {
-    unsigned char *to = lds + (u & 1) * C::STAGE;
-    const int first = tiles.at(u) * C::KT;
-    const bool careful = C::REST || !all_seen(first, C::KT, k.low, k.high);  // (an infinite value times a remainder of 0 or below is no infinity)
+  // marks: a value of the tile is not finite (of each of the waves that brought it)
+  auto careful_with = [&](int first) __attribute__((always_inline)) {  // (an infinite value times a remainder of 0 or below is no infinity)
+    return C::REST || !all_seen(first, C::KT, k.low, k.high);
+  };
+  auto stash = [&](int u, int stage) __attribute__((always_inline)) {
+    unsigned char *to = lds + stage * C::STAGE;
+    const bool careful = careful_with(tiles.at(u) * C::KT);
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
-      const int r = i * C::RPP + prow;
+      const int r = (i * C::TOGETHER + bring) * C::RPW + lrow;
       if constexpr (KIND == TVA_ROWS_BF16) {
         *(u32x4 *)(to + r * C::ROW + k_piece(r, piece) * 16) = kx[i];
         if (careful && not_finite(vx[i])) odd = true, vx[i] = finite_ones(vx[i]);
@@ -254,7 +286,7 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
     }
     if (careful) {
       const bool any = __any(odd);
-      if (lane == 0) odd_at[(u & 1) * C::WAVES + wave] = any;
+      if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = any;
     }
   };
 
@@ -264,14 +296,14 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
   float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
   f32x16 s[KB];
 
-  auto compute = [&](int u) __attribute__((always_inline)) {
-    const unsigned char *kt = lds + (u & 1) * C::STAGE + wk * C::KW * C::ROW, *vt = kt + C::TILE;
-    const int first = tiles.at(u) * C::KT, t0 = first + wk * C::KW;
-    // (a tile with a value that is not finite: all waves of the workgroup take the long way)
+  auto compute = [&](int u, int stage) __attribute__((always_inline)) {
+    const unsigned char *kt = lds + stage * C::STAGE + (C::OWN ? 0 : wk * C::KW * C::ROW), *vt = kt + C::TILE;
+    const int first = tiles.at(u) * C::KT, t0 = first + (C::OWN ? 0 : wk * C::KW);
+    // (a tile with a value that is not finite: all waves that have it take the long way)
     bool odd = false;
-    if (C::REST || !all_seen(first, C::KT, k.low, k.high)) {
+    if (careful_with(first)) {
 #pragma unroll
-      for (int w = 0; w < C::WAVES; ++w) odd |= odd_at[(u & 1) * C::WAVES + w] != 0;
+      for (int w = 0; w < C::TOGETHER; ++w) odd |= ((const int *)(lds + C::ODD))[C::OWN ? wave : stage * C::WAVES + w] != 0;
       odd = __builtin_amdgcn_readfirstlane(odd);
     }
     const bool masked = !all_seen(t0, C::KW, low, high);
@@ -290,6 +322,7 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[st], s[kb], 0, 0, 0);
       }
     if (masked) {
+      asm volatile("");  // (a branch: selects in every tile would cost as much as the exponentials)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const uint32_t bits = sees(t0 + kb * 32) >> (4 * half);
@@ -368,22 +401,42 @@ __global__ void __launch_bounds__(64 * WM *WK, (ChunkCfg<D, WM, WK, KB, KIND>::P
       }
   };
 
-  if (u0 < u1) {
+  if constexpr (C::OWN) {
+    int u = u0 + wk;
+    if (u < u1) {
+      look(u);
+      fetch(u);
+      look(u + C::STEP);
+      for (; u < u1; u += C::STEP) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        stash(u, wave);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        fetch(u + C::STEP);
+        look(u + 2 * C::STEP);
+        compute(u, wave);
+      }
+    }
+  } else if (u0 < u1) {
     look(u0);
     fetch(u0);
     look(u0 + 1);
-    stash(u0);
+    stash(u0, 0);
     fetch(u0 + 1);
     look(u0 + 2);
     __syncthreads();
-    for (int u = u0; u < u1; ++u) {
+    // (two tiles a turn, so that where a stage lies is a constant of the code)
+    auto step = [&](int u, auto stage) __attribute__((always_inline)) {
       if (u + 1 < u1) {
-        stash(u + 1);
+        stash(u + 1, 1 - stage.value);
         fetch(u + 2);
         look(u + 3);
       }
-      if (!idle) compute(u);
+      if (!idle) compute(u, stage.value);
       __syncthreads();
+    };
+    for (int u = u0; u < u1; u += 2) {
+      step(u, std::integral_constant<int, 0>{});
+      if (u + 1 < u1) step(u + 1, std::integral_constant<int, 1>{});
     }
   }
 
@@ -493,7 +546,7 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
   pl->rows = a->plan_rows ? a->plan_rows : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-  pl->KT = pl->rows == 32 ? 128 : 64;
+  pl->KT = pl->rows == 32 ? 32 : 64;
   const int64_t blocks = (int64_t)a->sum_T * G / pl->rows + a->B;
   pl->blocks = (int)std::min<int64_t>(blocks, 0x7fffffff);
   // keys that a row block may see
@@ -569,6 +622,7 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
   if (need && (!a->workspace || ((uintptr_t)a->workspace & 15))) return TVA_INVALID_ARG;
   if (a->workspace_bytes < need) return TVA_WORKSPACE_TOO_SMALL;
   if (pl.blocks > 65535 || pl.parts > 65535) return TVA_UNSUPPORTED;
+  if (p.c.stride_tok >= 1 << 25) return TVA_UNSUPPORTED;  // (offsets among the rows that a wave brings at once)
   const bool eight = a->cache.kind == TVA_ROWS_E4M3;
   const float k_scale = !eight || a->cache.k_scale == 0.f ? 1.f : a->cache.k_scale;
   p.q = (const __bf16 *)a->q, p.cu_T = a->cu_T, p.L = a->L, p.mask = a->anc_mask;
@@ -586,14 +640,16 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
     constexpr int D = decltype(d)::value, WM = decltype(wm)::value, WK = decltype(wk)::value, KB = decltype(kb)::value, THREADS = 64 * WM * WK;
     auto form = [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;
-      static_assert(32 * KB * WK == (WM == 1 ? 128 : 64), "plan_chunk");
-      if (a->cache.page_table) {
-        if (a->anc_mask) hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, true, true>), grid, dim3(THREADS), 0, st, p);
-        else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, true, false>), grid, dim3(THREADS), 0, st, p);
-      } else {
-        if (a->anc_mask) hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, false, true>), grid, dim3(THREADS), 0, st, p);
-        else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, false, false>), grid, dim3(THREADS), 0, st, p);
-      }
+      typedef ChunkCfg<D, WM, WK, KB, KIND> C;
+      static_assert(C::KT == (WM == 1 ? 32 : 64), "plan_chunk");
+      auto go = [&](auto places) {
+        constexpr int PLACES = decltype(places)::value;
+        if (a->anc_mask) hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, PLACES, true>), grid, dim3(THREADS), 0, st, p);
+        else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, PLACES, false>), grid, dim3(THREADS), 0, st, p);
+      };
+      if (!a->cache.page_table) go(std::integral_constant<int, kDense>{});
+      else if (a->cache.page_size % C::RPW == 0) go(std::integral_constant<int, kPages>{});
+      else go(std::integral_constant<int, kRows>{});
     };
     if (eight) form(std::integral_constant<int, TVA_ROWS_E4M3>{});
     else form(std::integral_constant<int, TVA_ROWS_BF16>{});

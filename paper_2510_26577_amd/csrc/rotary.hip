@@ -121,13 +121,12 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
   }
 
   // ---- the token's place and position ----
-  int b = 0, i = (int)row, P = 0;
+  int b = 0, i = (int)row, P = 0, start = 0;
   if (p.cu_T) {
-    b = sequences::find(p.B, [&](int n) { return p.cu_T[n] <= row; });
-    i = (int)row - p.cu_T[b];
-    if (i < 0 || (int)row >= p.cu_T[b + 1]) return;  // behind the last sequence
+    const sequences::Place at = sequences::find(p.cu_T, p.L, p.B, row, [](int, int from) { return (int64_t)from; });
+    b = at.b, i = (int)row - at.t0, start = at.L;
+    if (i < 0 || (int)row >= at.t1) return;  // behind the last sequence
   }
-  const int start = KIND != kNoCache || !p.pos ? p.L[b] : 0;
   if (p.pos) {
     P = p.pos[row];
   } else if (p.mask) {
