@@ -113,7 +113,7 @@ typedef struct tva_chunk_args {
   int32_t window, n_first;      /* 0 = no window (n_first is then ignored) */
   float scale;                  /* > 0 */
   int32_t num_splits;           /* the most parts a row block's keys are split into; 0 = the library chooses */
-  int32_t plan_rows;            /* query rows (tokens x heads of a KV head) per workgroup: 32, 64, 128 or 256; 0 = the library
+  int32_t plan_rows;            /* query rows (tokens x heads of a KV head) per workgroup: 32, 128 or 256; 0 = the library
                                    chooses.  A tuning and testing aid: every value computes the same, to the roundings above */
   int32_t reserved;
   const int32_t *cu_T, *L;      /* device [B+1], [B] */

@@ -117,8 +117,11 @@ struct ChunkCfg {
   static constexpr int R = 32 * WM, KW = 32 * KB, KT = OWN ? KW : KW * WK;  // rows; keys of a tile that a wave multiplies, and of a tile
   static constexpr int STEP = OWN ? WK : 1;                                // tiles from one of a wave's to its next
   static constexpr int NS = D / 16, NJ = D / 32;
-  static constexpr int ROW = 2 * D, TILE = KT * ROW, STAGE = 2 * TILE;  // bytes in LDS
-  static constexpr int STAGES = OWN ? WK : 2;
+  // Bytes from row to row in LDS: spaced so that 16 rows of K at one 16-byte piece each, and four rows of V at 64 bytes of each, are in
+  // different banks, and an operand's address is one register and constants.
+  static constexpr int K_ROW = 2 * D + 16, V_ROW = 2 * D + 64;
+  static constexpr int STAGES = OWN ? WK : 2;  // of K, and as many of V
+  static constexpr int K_TILE = KT * K_ROW, V_TILE = KT * V_ROW;
   static constexpr int TOGETHER = OWN ? 1 : WAVES;                        // waves that bring a tile
   static constexpr int EPL = KIND == TVA_ROWS_BF16 || KT * D / 16 < 64 * TOGETHER ? 8 : 16;  // elements that a lane brings at once
   static constexpr int LPR = D / EPL, RPW = 64 / LPR;                     // lanes that bring a row, rows that a wave brings at once
@@ -126,7 +129,7 @@ struct ChunkCfg {
   static_assert(KT % (RPW * TOGETHER) == 0, "");
   static constexpr int TP = D + 4, PATCH = 32 * TP * 4;  // an output patch per wave, floats between its rows
   static constexpr int EXCHANGE = 2 * WAVES * 32 * 4;
-  static constexpr int DEPTH = STAGES * STAGE, ODD = DEPTH + TVA_MAX_TREE * 4;  // LDS: tiles, depths of a tree's nodes, marks of tiles
+  static constexpr int DEPTH = STAGES * (K_TILE + V_TILE), ODD = DEPTH + TVA_MAX_TREE * 4;  // LDS: tiles, depths of a tree's nodes, marks of tiles
   static constexpr int LOOP_LDS = ODD + 2 * WAVES * 4, END_LDS = WAVES * PATCH + EXCHANGE;
   static constexpr int LDS = LOOP_LDS > END_LDS ? LOOP_LDS : END_LDS;
   // remainders of the softmax weights are multiplied too (their rounding to bf16 would show; the shape waits for memory)
@@ -219,6 +222,8 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   constexpr int BYTES = KIND == TVA_ROWS_BF16 ? 2 : 1;            // of an element
   u32x4 kx[C::NP], vx[C::NP];
   int entry[PLACES == kRows ? C::NP : 1];  // kRows: the page of this lane's row of each read; kPages: lane i has that of read i
+  int64_t place[C::NP];                    // of the reads of K's tile, in bytes: V's are the same, later
+  uint32_t within[C::NP];
   // (a tile past the last one: the last again.  A branch would leave the waits without a count to go by)
   auto first_slot = [&](int u) __attribute__((always_inline)) { return tiles.at(min(u, u1 - 1)) * C::KT; };
   auto look = [&](int u) __attribute__((always_inline)) {
@@ -230,58 +235,64 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       entry[0] = find.entry(p.c, min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group));
     }
   };
-  auto fetch = [&](int u) __attribute__((always_inline)) {
+  auto locate = [&](int u) __attribute__((always_inline)) {
     const int t = first_slot(u);
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
-      const char *from_k, *from_v;
       if constexpr (PLACES == kRows) {
-        const int row = min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last);
-        const int64_t at = (find.at(p.c, row, entry[i]) + piece * C::EPL) * BYTES;
-        from_k = p.c.k + at, from_v = p.c.v + at;
+        place[i] = find.at(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last), entry[i]) * BYTES;
+        within[i] = piece * C::EPL * BYTES;
       } else {
         const int row = min(t + (i * C::TOGETHER + bring) * C::RPW, last_group);
-        int64_t at;
-        if constexpr (PLACES == kPages) at = find.at(p.c, row, __builtin_amdgcn_readlane(entry[0], i)) * BYTES;
-        else at = find.at(p.c, row, 0) * BYTES;
-        const uint32_t off = (uint32_t)min(lrow, last - row) * (uint32_t)(p.c.stride_tok * BYTES) + (uint32_t)(piece * C::EPL * BYTES);
-        from_k = p.c.k + at + off, from_v = p.c.v + at + off;
-      }
-      if constexpr (C::EPL * BYTES == 16) {
-        kx[i] = *(const u32x4 *)from_k, vx[i] = *(const u32x4 *)from_v;
-      } else {
-        const u32x2 a = *(const u32x2 *)from_k, b = *(const u32x2 *)from_v;
-        kx[i] = u32x4{a[0], a[1], 0, 0}, vx[i] = u32x4{b[0], b[1], 0, 0};
+        place[i] = find.at(p.c, row, PLACES == kPages ? __builtin_amdgcn_readlane(entry[0], i) : 0) * BYTES;
+        within[i] = (uint32_t)min(lrow, last - row) * (uint32_t)(p.c.stride_tok * BYTES) + (uint32_t)(piece * C::EPL * BYTES);
       }
     }
   };
-  // Where 16-byte piece c of row r lies in its row, so that the lanes of a read are in different banks: 16 rows of K at one piece each; of V
-  // four consecutive rows, 64 bytes of each.
-  auto k_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); };
-  auto v_piece = [](int r, int c) __attribute__((always_inline)) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); };
-  // marks: a value of the tile is not finite (of each of the waves that brought it)
-  auto careful_with = [&](int first) __attribute__((always_inline)) {  // (an infinite value times a remainder of 0 or below is no infinity)
-    return C::REST || !all_seen(first, C::KT, k.low, k.high);
+  auto read = [&](u32x4 (&x)[C::NP], const char *from) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::NP; ++i) {
+      if constexpr (C::EPL * BYTES == 16) {
+        x[i] = *(const u32x4 *)(from + place[i] + within[i]);
+      } else {
+        const u32x2 a = *(const u32x2 *)(from + place[i] + within[i]);
+        x[i] = u32x4{a[0], a[1], 0, 0};
+      }
+    }
   };
-  auto stash = [&](int u, int stage) __attribute__((always_inline)) {
-    unsigned char *to = lds + stage * C::STAGE;
-    const bool careful = careful_with(tiles.at(u) * C::KT);
-    bool odd = false;
+  auto k_stage = [&](int stage) __attribute__((always_inline)) { return lds + stage * C::K_TILE; };
+  auto v_stage = [&](int stage) __attribute__((always_inline)) { return lds + C::STAGES * C::K_TILE + stage * C::V_TILE; };
+  // Tiles that some row does not see all of are looked through for values that are not finite: those go to LDS as 0 (a weight of 0 times
+  // them is no 0), the tile is marked, and rows that see them get them added.  (With remainders every tile: an infinite value times a
+  // remainder of 0 or below is no infinity.)
+  auto careful_with = [&](int u) __attribute__((always_inline)) { return C::REST || !all_seen(tiles.at(u) * C::KT, C::KT, k.low, k.high); };
+  auto stash_k = [&](int stage) __attribute__((always_inline)) {
+    unsigned char *to = k_stage(stage);
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
       const int r = (i * C::TOGETHER + bring) * C::RPW + lrow;
       if constexpr (KIND == TVA_ROWS_BF16) {
-        *(u32x4 *)(to + r * C::ROW + k_piece(r, piece) * 16) = kx[i];
-        if (careful && not_finite(vx[i])) odd = true, vx[i] = finite_ones(vx[i]);
-        *(u32x4 *)(to + C::TILE + r * C::ROW + v_piece(r, piece) * 16) = vx[i];
+        *(u32x4 *)(to + r * C::K_ROW + piece * 16) = kx[i];
       } else {
 #pragma unroll
-        for (int h = 0; h < C::EPL / 8; ++h) {
-          *(bf16x8 *)(to + r * C::ROW + k_piece(r, C::EPL / 8 * piece + h) * 16) = widen8_e4m3(u32x2{kx[i][2 * h], kx[i][2 * h + 1]});
-          u32x4 v = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i][2 * h], vx[i][2 * h + 1]}));
-          if (careful && not_finite(v)) odd = true, v = finite_ones(v);
-          *(u32x4 *)(to + C::TILE + r * C::ROW + v_piece(r, C::EPL / 8 * piece + h) * 16) = v;
-        }
+        for (int h = 0; h < C::EPL / 8; ++h)
+          *(bf16x8 *)(to + r * C::K_ROW + (C::EPL / 8 * piece + h) * 16) = widen8_e4m3(u32x2{kx[i][2 * h], kx[i][2 * h + 1]});
+      }
+    }
+  };
+  auto stash_v = [&](int u, int stage) __attribute__((always_inline)) {
+    unsigned char *to = v_stage(stage);
+    const bool careful = careful_with(u);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < C::NP; ++i) {
+      const int r = (i * C::TOGETHER + bring) * C::RPW + lrow;
+#pragma unroll
+      for (int h = 0; h < (KIND == TVA_ROWS_BF16 ? 1 : C::EPL / 8); ++h) {
+        u32x4 v = vx[i];
+        if constexpr (KIND != TVA_ROWS_BF16) v = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i][2 * h], vx[i][2 * h + 1]}));
+        if (careful && not_finite(v)) odd = true, v = finite_ones(v);
+        *(u32x4 *)(to + r * C::V_ROW + (C::EPL / 8 * piece + h) * 16) = v;
       }
     }
     if (careful) {
@@ -289,154 +300,222 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = any;
     }
   };
+  auto is_odd = [&](int u, int stage) __attribute__((always_inline)) -> bool {
+    bool odd = false;
+    if (careful_with(u)) {
+#pragma unroll
+      for (int w = 0; w < C::TOGETHER; ++w) odd |= ((const int *)(lds + C::ODD))[C::OWN ? wave : stage * C::WAVES + w] != 0;
+    }
+    return same(odd);
+  };
 
   f32x16 acc[C::NJ];
 #pragma unroll
   for (int j = 0; j < C::NJ; ++j) acc[j] = f32x16{};
   float m = -INFINITY, l = 0.f;  // reference (log2 domain) and sum over this lane half's keys
-  f32x16 s[KB];
 
-  auto compute = [&](int u, int stage) __attribute__((always_inline)) {
-    const unsigned char *kt = lds + stage * C::STAGE + (C::OWN ? 0 : wk * C::KW * C::ROW), *vt = kt + C::TILE;
-    const int first = tiles.at(u) * C::KT, t0 = first + (C::OWN ? 0 : wk * C::KW);
-    // (a tile with a value that is not finite: all waves that have it take the long way)
-    bool odd = false;
-    if (careful_with(first)) {
+  // ---- what is done with 32 keys ----
+  // S^T = K Q^T, of which row l32 of K is this lane's operand
+  auto k_operand = [&](const unsigned char *kt, int kb, int st) __attribute__((always_inline)) {
+    return *(const bf16x8 *)(kt + (kb * 32 + l32) * C::K_ROW + (st * 2 + half) * 16);
+  };
+  // O^T += V^T P^T, of 16 keys and 32 elements: 16 lanes turn over 4 rows x 16 elements, this lane's row (of keys 8 h + 4 half + 0..3) and 8-byte
+  // piece of it
+  const int i16 = lane & 15, sub = (lane >> 4) & 1;
+  auto v_operand = [&](const unsigned char *vt, int kb, int a, int j) __attribute__((always_inline)) {
+    s16x4 c[2];
 #pragma unroll
-      for (int w = 0; w < C::TOGETHER; ++w) odd |= ((const int *)(lds + C::ODD))[C::OWN ? wave : stage * C::WAVES + w] != 0;
-      odd = __builtin_amdgcn_readfirstlane(odd);
+    for (int h = 0; h < 2; ++h) {
+      const int r = 32 * kb + 16 * a + 8 * h + 4 * half + (i16 >> 2);
+      c[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4 *)(vt + r * C::V_ROW + j * 64 + sub * 32 + (i16 & 3) * 8));
     }
-    const bool masked = !all_seen(t0, C::KW, low, high);
-    if (masked) {
-      const bool none = t0 >= k.end || (!TREE && t0 > high) || (t0 + C::KW - 1 <= low - p.window && t0 >= p.n_first && (!TREE || t0 + C::KW <= k.L));
-      if (none) return;
-    }
-    // ---- S^T = K Q^T
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto mask = [&](f32x16 &s, int t) __attribute__((always_inline)) {
+    const uint32_t bits = sees(t) >> (4 * half);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
-#pragma unroll
-    for (int st = 0; st < C::NS; ++st)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const bf16x8 x = *(const bf16x8 *)(kt + (kb * 32 + l32) * C::ROW + k_piece(l32, st * 2 + half) * 16);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[st], s[kb], 0, 0, 0);
-      }
-    if (masked) {
-      asm volatile("");  // (a branch: selects in every tile would cost as much as the exponentials)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const uint32_t bits = sees(t0 + kb * 32) >> (4 * half);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[kb][i] = -INFINITY;
-      }
-    }
-    // ---- scores -> weights in place; O and l move to a new reference where a row's largest score exceeds it by more than 2^8
-    float top = s[0][0];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-    top = half_max(top) * p.scale_log2;
-    if (__any(top > m + 8.f)) {
-      const float to = fmaxf(m, top);
-      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-      m = to, l *= f;
+    for (int i = 0; i < 16; ++i)
+      if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[i] = -INFINITY;
+  };
+  auto add_odd = [&](int t0) __attribute__((always_inline)) {
+    for (int t = t0; t < min(t0 + 32, k.end); ++t) {
+      const bool here = sees(t) & 1;
+      const int64_t at = find.at(p.c, t, find.entry(p.c, t));
 #pragma unroll
       for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[j][i] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, -ref));
-        l += s[kb][i];
-      }
-    // ---- O^T += V^T P^T: 16 lanes turn over 4 rows x 16 elements: this lane's row (of keys 8 h + 4 half + 0..3) and 8-byte piece of it
-    const int i16 = lane & 15, sub = (lane >> 4) & 1;
-    if (odd) {  // what is not finite was taken out of the tile: rows that see it get it added
-      for (int x = 0; x < C::KW; ++x) {
-        const int t = t0 + x;
-        if (t >= k.end) break;
-        const bool here = sees(t) & 1;
-        const int64_t at = find.at(p.c, t, find.entry(p.c, t));
-#pragma unroll
-        for (int j = 0; j < C::NJ; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int d = 32 * j + 8 * (i / 4) + 4 * half + i % 4;
-            float v;
-            if constexpr (KIND == TVA_ROWS_BF16) v = (float)((const __bf16 *)p.c.v)[at + d];
-            else v = (((const uint8_t *)p.c.v)[at + d] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
-            if (here && !__builtin_isfinite(v)) acc[j][i] += v;
-          }
-      }
-    }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        bf16x8 w, rest;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          w[i] = (__bf16)s[kb][a * 8 + i];
-          if constexpr (C::REST) rest[i] = (__bf16)(s[kb][a * 8 + i] - (float)w[i]);
+        for (int i = 0; i < 16; ++i) {
+          const int d = 32 * j + 8 * (i / 4) + 4 * half + i % 4;
+          float v;
+          if constexpr (KIND == TVA_ROWS_BF16) v = (float)((const __bf16 *)p.c.v)[at + d];
+          else v = (((const uint8_t *)p.c.v)[at + d] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+          if (here && !__builtin_isfinite(v)) acc[j][i] += v;
         }
+    }
+  };
+  // A row's largest score (log2 domain) of 32 N keys; and whether the reference is to move: only where it is exceeded by more than 2^8, and
+  // then for all rows of the wave.  Moving it brings l and O along.
+  auto top_of = [&](auto &...s) __attribute__((always_inline)) -> float {
+    float top = -INFINITY;
+    auto take = [&](const f32x16 &x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < C::NJ; ++j) {
-          s16x4 c[2];
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
+    };
+    (take(s), ...);
+    return half_max(top) * p.scale_log2;
+  };
+  auto moves = [&](float top) __attribute__((always_inline)) -> bool { return __any(top > m + 8.f); };
+  auto move_to = [&](float top) __attribute__((always_inline)) {
+    const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+    m = to, l *= f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = 32 * kb + 16 * a + 8 * h + 4 * half + (i16 >> 2);
-            c[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4 *)(vt + r * C::ROW + v_piece(i16 >> 2, j * 4 + sub * 2) * 16 + (i16 & 3) * 8));
-          }
-          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(c[0], c[1], 0, 1, 2, 3, 4, 5, 6, 7));
-          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[j], 0, 0, 0);
-          if constexpr (C::REST) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest, acc[j], 0, 0, 0);
-        }
-      }
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[j][i] *= f;
+  };
+  // Scores -> weights (bf16, and what their rounding leaves), their sum added to l
+  auto soften = [&](const f32x16 &s, float ref, bf16x8 (&w)[2], bf16x8 (&rest)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -ref));
+      l += x;
+      w[i / 8][i % 8] = (__bf16)x;
+      if constexpr (C::REST) rest[i / 8][i % 8] = (__bf16)(x - (float)w[i / 8][i % 8]);
+    }
   };
 
   if constexpr (C::OWN) {
+    static_assert(KB == 1, "");
     int u = u0 + wk;
     if (u < u1) {
       look(u);
-      fetch(u);
+      locate(u);
+      read(kx, p.c.k), read(vx, p.c.v);
       look(u + C::STEP);
       for (; u < u1; u += C::STEP) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        stash(u, wave);
+        stash_k(wave);
+        stash_v(u, wave);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        fetch(u + C::STEP);
+        locate(u + C::STEP);
+        read(kx, p.c.k), read(vx, p.c.v);
         look(u + 2 * C::STEP);
-        compute(u, wave);
+        const int t = tiles.at(u) * C::KT;
+        const bool masked = !all_seen(t, 32, low, high);
+        f32x16 s = {};
+#pragma unroll
+        for (int st = 0; st < C::NS; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k_stage(wave), 0, st), q[st], s, 0, 0, 0);
+        if (masked) mask(s, t);
+        const float top = top_of(s);
+        if (moves(top)) move_to(top);
+        bf16x8 w[2], rest[2];
+        soften(s, m == -INFINITY ? 0.f : m, w, rest);
+        if (is_odd(u, wave)) add_odd(t);
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int j = 0; j < C::NJ; ++j) {
+            const bf16x8 v = v_operand(v_stage(wave), 0, a, j);
+            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[a], acc[j], 0, 0, 0);
+            if constexpr (C::REST) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[a], acc[j], 0, 0, 0);
+          }
       }
     }
   } else if (u0 < u1) {
-    look(u0);
-    fetch(u0);
-    look(u0 + 1);
-    stash(u0, 0);
-    fetch(u0 + 1);
-    look(u0 + 2);
-    __syncthreads();
-    // (two tiles a turn, so that where a stage lies is a constant of the code)
-    auto step = [&](int u, auto stage) __attribute__((always_inline)) {
-      if (u + 1 < u1) {
-        stash(u + 1, 1 - stage.value);
-        fetch(u + 2);
-        look(u + 3);
-      }
-      if (!idle) compute(u, stage.value);
-      __syncthreads();
+    static_assert(KB == 2 && WK == 1, "");
+    // Beside the softmax of tile u run the products of tile u + 1's scores, beside those of O with tile u the search for tile u + 1's largest
+    // scores: matrix and vector instructions of a wave that do not wait for each other.  K's tiles are therefore a tile ahead of V's.
+    f32x16 s[2], next[2];
+    auto scores = [&](int stage, f32x16 (&s)[2]) __attribute__((always_inline)) {
+      const unsigned char *kt = k_stage(stage);
+      s[0] = f32x16{}, s[1] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < C::NS; ++st)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(kt, kb, st), q[st], s[kb], 0, 0, 0);
     };
-    for (int u = u0; u < u1; u += 2) {
-      step(u, std::integral_constant<int, 0>{});
-      if (u + 1 < u1) step(u + 1, std::integral_constant<int, 1>{});
+    auto products = [&](int stage, int kb, const bf16x8 (&w)[2]) __attribute__((always_inline)) {
+      const unsigned char *vt = v_stage(stage);
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vt, kb, a, j), w[a], acc[j], 0, 0, 0);
+    };
+    // K of tile u + 2 takes the place of tile u's, V of tile u + 1 that of tile u - 1's
+    auto bring = [&](int u) __attribute__((always_inline)) {
+      stash_k(u & 1);
+      stash_v(u + 1, 1 - (u & 1));
+      read(vx, p.c.v);  // of tile u + 2
+      locate(u + 3);
+      read(kx, p.c.k);
+      look(u + 4);
+    };
+    // tiles without marks that all rows of the wave see
+    auto plain = [&](int u) __attribute__((always_inline)) { return !careful_with(u) && all_seen(tiles.at(u) * C::KT, C::KT, low, high); };
+    look(u0);
+    locate(u0);
+    read(kx, p.c.k), read(vx, p.c.v);
+    look(u0 + 1);
+    stash_k(u0 & 1), stash_v(u0, u0 & 1);
+    locate(u0 + 1);
+    look(u0 + 2);
+    read(kx, p.c.k);
+    stash_k(1 - (u0 & 1));
+    read(vx, p.c.v);
+    locate(u0 + 2);
+    look(u0 + 3);
+    read(kx, p.c.k);
+    __syncthreads();
+    float top = -INFINITY;  // of s
+    if (!idle) {
+      scores(u0 & 1, s);
+      const int t = tiles.at(u0) * C::KT;
+      if (!all_seen(t, C::KT, low, high)) mask(s[0], t), mask(s[1], t + 32);
+      top = top_of(s[0], s[1]);
+    }
+    __syncthreads();  // (K's first tile has been read)
+    int u = u0;
+    while (true) {
+      if (moves(top)) move_to(top);
+      // as long as there is nothing out of the ordinary, straight ahead
+      while (!idle && u + 1 < u1 && plain(u) && plain(u + 1)) {
+        bring(u);
+        const float ref = m;
+        bf16x8 w[2][2], rest[2];
+        scores(1 - (u & 1), next);
+        soften(s[0], ref, w[0], rest);
+        soften(s[1], ref, w[1], rest);
+        products(u & 1, 0, w[0]);
+        products(u & 1, 1, w[1]);
+        top = top_of(next[0], next[1]);
+        s[0] = next[0], s[1] = next[1];
+        ++u;
+        __syncthreads();
+        if (moves(top)) break;
+      }
+      if (moves(top)) move_to(top);
+      if (u + 1 < u1) bring(u);
+      if (!idle) {
+        const float ref = m == -INFINITY ? 0.f : m;
+        const int t = tiles.at(u) * C::KT;
+        const bool odd = is_odd(u, u & 1);
+        bf16x8 w[2], rest[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          soften(s[kb], ref, w, rest);
+          if (odd) add_odd(t + 32 * kb);
+          products(u & 1, kb, w);
+        }
+        if (u + 1 < u1) {
+          scores(1 - (u & 1), s);
+          const int t = tiles.at(u + 1) * C::KT;
+          if (!all_seen(t, C::KT, low, high)) mask(s[0], t), mask(s[1], t + 32);
+          top = top_of(s[0], s[1]);
+        }
+      }
+      if (++u >= u1) break;
+      __syncthreads();
     }
   }
 
@@ -545,14 +624,14 @@ struct ChunkPlan {
 void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
-  pl->rows = a->plan_rows ? a->plan_rows : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  pl->rows = a->plan_rows ? a->plan_rows : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   pl->KT = pl->rows == 32 ? 32 : 64;
   const int64_t blocks = (int64_t)a->sum_T * G / pl->rows + a->B;
   pl->blocks = (int)std::min<int64_t>(blocks, 0x7fffffff);
   // keys that a row block may see
   const int64_t seen = a->window ? std::min<int64_t>((int64_t)a->max_L + a->max_T, (int64_t)a->window + a->n_first + pl->rows / G + 2 * pl->KT) : (int64_t)a->max_L + a->max_T;
   const int64_t tiles = std::max<int64_t>(1, (seen + pl->KT - 1) / pl->KT);
-  const int slots = pl->rows == 32 || pl->rows == 256 ? 256 : 512;
+  const int slots = pl->rows == 256 ? 256 : 512;
   // row blocks that have rows: a sequence of max_T tokens has this many
   const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(blocks, (int64_t)a->B * ((rows + pl->rows - 1) / pl->rows))) * a->Hkv;
   int64_t parts = a->num_splits;
@@ -566,7 +645,7 @@ int check_chunk(const tva_chunk_args *a, bool shapes_only) {
   if (!a || a->B <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv) return TVA_INVALID_ARG;
   if (a->sum_T < 0 || a->max_T < 0 || a->max_L < 0 || a->num_splits < 0 || a->window < 0 || a->n_first < 0) return TVA_INVALID_ARG;
   if (a->D != 64 && a->D != 128) return TVA_UNSUPPORTED;
-  if (a->plan_rows != 0 && a->plan_rows != 32 && a->plan_rows != 64 && a->plan_rows != 128 && a->plan_rows != 256) return TVA_INVALID_ARG;
+  if (a->plan_rows != 0 && a->plan_rows != 32 && a->plan_rows != 128 && a->plan_rows != 256) return TVA_INVALID_ARG;
   if (a->max_L > 1 << 29 || a->max_T > 1 << 28 || (int64_t)a->max_T * (a->Hq / a->Hkv) > 1 << 30) return TVA_UNSUPPORTED;  // (positions below 2^30)
   if (a->anc_mask && (a->max_T > TVA_MAX_TREE || a->mask_words < 1 || a->mask_words > 2 || a->mask_words * 64 < a->max_T)) return TVA_UNSUPPORTED;
   if (shapes_only) return TVA_OK;
@@ -662,7 +741,6 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
   typedef std::integral_constant<int, 8> many;
   auto shapes = [&](auto d) {
     if (pl.rows == 32) launch(d, one{}, four{}, one{});
-    else if (pl.rows == 64) launch(d, two{}, two{}, one{});
     else if (pl.rows == 128) launch(d, four{}, one{}, two{});
     else launch(d, many{}, one{}, two{});
   };
