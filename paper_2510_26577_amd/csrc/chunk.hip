@@ -136,6 +136,12 @@ struct ChunkCfg {
   static constexpr bool REST = WM == 1;
 };
 
+template <int N, class F>
+__device__ __forceinline__ void times(F f) {
+  if constexpr (N > 0) times<N - 1>(f), f(std::integral_constant<int, N - 1>{});
+}
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block (the last ones, which see the
 // most keys, first).
 // PLACES: how a tile's rows are found.  kDense and kPages: the rows that a wave brings at once lie in a sequence, or a page, one after the
@@ -214,6 +220,15 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   auto all_seen = [&](int t, int n, int low, int high) __attribute__((always_inline)) -> bool {
     return t + n <= k.end && t + n - 1 <= (TREE ? k.L - 1 : low) && (t > high - p.window || t + n <= p.n_first);
   };
+  // the tiles all of which all those rows see, but for any of the first ones: a run of them
+  auto run_of = [&](int low, int high, int *from, int *to) __attribute__((always_inline)) {
+    const int whole = min(k.end, (TREE ? k.L : low + 1)) / C::KT;               // tiles below it end before what some row does not see
+    const int near = max(high - p.window + C::KT, 0) / C::KT;                   // tiles from it on begin in all windows
+    *from = same(max(near, tiles.main) - tiles.main + tiles.first), *to = same(whole - tiles.main + tiles.first);
+  };
+  int quiet0, quiet1, plain0, plain1;  // of the workgroup's rows, of the wave's
+  run_of(k.low, k.high, &quiet0, &quiet1);
+  run_of(low, high, &plain0, &plain1);
 
   // ---- tiles: global memory -> registers -> LDS ----
   const Finder<PLACES != kDense> find(p.c, k.b, g);
@@ -221,9 +236,11 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   const int last = k.end - 1, last_group = last - last % C::RPW;  // the last slot, and the first of the group that it is in
   constexpr int BYTES = KIND == TVA_ROWS_BF16 ? 2 : 1;            // of an element
   u32x4 kx[C::NP], vx[C::NP];
-  int entry[PLACES == kRows ? C::NP : 1];  // kRows: the page of this lane's row of each read; kPages: lane i has that of read i
+  int entry[PLACES == kRows ? C::NP : 1];  // kRows: the page of this lane's row of each read; kPages: lane i has that of read i, and
+  uint32_t in_page = 0;                    // where its rows begin in the page, in bytes
   int64_t place[C::NP];                    // of the reads of K's tile, in bytes: V's are the same, later
   uint32_t within[C::NP];
+  const uint32_t row_bytes = (uint32_t)(p.c.stride_tok * BYTES);
   // (a tile past the last one: the last again.  A branch would leave the waits without a count to go by)
   auto first_slot = [&](int u) __attribute__((always_inline)) { return tiles.at(min(u, u1 - 1)) * C::KT; };
   auto look = [&](int u) __attribute__((always_inline)) {
@@ -232,20 +249,26 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
 #pragma unroll
       for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last));
     } else if constexpr (PLACES == kPages) {
-      entry[0] = find.entry(p.c, min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group));
+      const int row = min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group), page = page_of(p.c, row);
+      entry[0] = find.table[page], in_page = (uint32_t)(row - page * p.c.page_size) * row_bytes;
     }
   };
   auto locate = [&](int u) __attribute__((always_inline)) {
     const int t = first_slot(u);
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
+      const int row = t + (i * C::TOGETHER + bring) * C::RPW;
       if constexpr (PLACES == kRows) {
-        place[i] = find.at(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last), entry[i]) * BYTES;
+        place[i] = find.at(p.c, min(row + lrow, last), entry[i]) * BYTES;
         within[i] = piece * C::EPL * BYTES;
+      } else if constexpr (PLACES == kPages) {
+        // (the launch sees to it that a page has less than 2^32 bytes)
+        place[i] = find.base * BYTES + (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(entry[0], i) * (uint32_t)(p.c.stride_page * BYTES)) +
+                   (uint32_t)__builtin_amdgcn_readlane((int)in_page, i);
+        within[i] = (uint32_t)min(lrow, last - min(row, last_group)) * row_bytes + (uint32_t)(piece * C::EPL * BYTES);
       } else {
-        const int row = min(t + (i * C::TOGETHER + bring) * C::RPW, last_group);
-        place[i] = find.at(p.c, row, PLACES == kPages ? __builtin_amdgcn_readlane(entry[0], i) : 0) * BYTES;
-        within[i] = (uint32_t)min(lrow, last - row) * (uint32_t)(p.c.stride_tok * BYTES) + (uint32_t)(piece * C::EPL * BYTES);
+        place[i] = find.base * BYTES + (int64_t)((uint64_t)(uint32_t)t * row_bytes);
+        within[i] = (uint32_t)min((i * C::TOGETHER + bring) * C::RPW + lrow, last - t) * row_bytes + (uint32_t)(piece * C::EPL * BYTES);
       }
     }
   };
@@ -265,7 +288,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   // Tiles that some row does not see all of are looked through for values that are not finite: those go to LDS as 0 (a weight of 0 times
   // them is no 0), the tile is marked, and rows that see them get them added.  (With remainders every tile: an infinite value times a
   // remainder of 0 or below is no infinity.)
-  auto careful_with = [&](int u) __attribute__((always_inline)) { return C::REST || !all_seen(tiles.at(u) * C::KT, C::KT, k.low, k.high); };
+  auto careful_with = [&](int u) __attribute__((always_inline)) { return C::REST || u < quiet0 || u >= quiet1; };
   auto stash_k = [&](int stage) __attribute__((always_inline)) {
     unsigned char *to = k_stage(stage);
 #pragma unroll
@@ -426,7 +449,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     static_assert(KB == 2 && WK == 1, "");
     // Beside the softmax of tile u run the products of tile u + 1's scores, beside those of O with tile u the search for tile u + 1's largest
     // scores: matrix and vector instructions of a wave that do not wait for each other.  K's tiles are therefore a tile ahead of V's.
-    f32x16 s[2], next[2];
+    f32x16 s[2], next;
     auto scores = [&](int stage, f32x16 (&s)[2]) __attribute__((always_inline)) {
       const unsigned char *kt = k_stage(stage);
       s[0] = f32x16{}, s[1] = f32x16{};
@@ -451,8 +474,6 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       read(kx, p.c.k);
       look(u + 4);
     };
-    // tiles without marks that all rows of the wave see
-    auto plain = [&](int u) __attribute__((always_inline)) { return !careful_with(u) && all_seen(tiles.at(u) * C::KT, C::KT, low, high); };
     look(u0);
     locate(u0);
     read(kx, p.c.k), read(vx, p.c.v);
@@ -475,23 +496,75 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       top = top_of(s[0], s[1]);
     }
     __syncthreads();  // (K's first tile has been read)
+    // tiles without marks, the next one too and seen by all rows of the wave: tile u of those below `until`
+    const int from = max(quiet0, plain0), until = idle ? 0 : min(min(quiet1, plain1), u1) - 1;
+    auto ahead = [&](int u) __attribute__((always_inline)) { return u >= from && u < until; };
+    // A tile in the order in which it runs (left to itself the compiler has all products first and their operands' reads right before them):
+    // per matrix instruction the softmax of EACH scores, in three steps of which each waits for none of its own turn, and an operand read AHEAD
+    // matrix instructions ahead.  x holds the scores of half h of tile u, y those of the other; z takes those of half h of tile u + 1, then x
+    // those of the other.
+    //   scores z     | weights of x
+    //   O with x's   | weights of y
+    //   scores x     | largest of z
+    //   O with y's   | largest of x
+    constexpr int NS = C::NS, NP = 2 * C::NJ, AHEAD = 4, EACH = 16 / NS;
+    static_assert(NS == NP, "");
+    auto straight = [&](int u, f32x16 &x, f32x16 &y, f32x16 &z, auto h) __attribute__((always_inline)) {
+      constexpr int H = decltype(h)::value;
+      bring(u);
+      const float ref = m;
+      const unsigned char *kt = k_stage(1 - (u & 1)), *vt = v_stage(u & 1);
+      bf16x8 ops[AHEAD], w[2][2];
+      float arg[2][EACH], e[2][EACH];
+      top = -INFINITY;
+      auto fetch = [&](auto i) __attribute__((always_inline)) {  // of matrix instruction i
+        constexpr int I = decltype(i)::value, PART = I / NS, N = I % NS, HALF = PART < 2 ? H : 1 - H;
+        if constexpr (PART == 0 || PART == 2) ops[I % AHEAD] = k_operand(kt, HALF, N);
+        else if constexpr (PART < 4) ops[I % AHEAD] = v_operand(vt, HALF, N / C::NJ, N % C::NJ);
+      };
+      times<AHEAD>(fetch);
+      in_order();
+      times<4 * NS>([&](auto i) __attribute__((always_inline)) {
+        constexpr int I = decltype(i)::value, PART = I / NS, N = I % NS;
+        const bf16x8 op = ops[I % AHEAD];
+        if constexpr (PART == 0) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, q[N], N == 0 ? f32x16{} : z, 0, 0, 0);
+        else if constexpr (PART == 2) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, q[N], N == 0 ? f32x16{} : x, 0, 0, 0);
+        else acc[N % C::NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, w[PART / 2][N / C::NJ], acc[N % C::NJ], 0, 0, 0);
+        fetch(std::integral_constant<int, I + AHEAD>{});
+        // arguments of turn I, exponentials of turn I - 1, sums and roundings of turn I - 2 (a half's last ones are done in the next part's first turns)
+        if constexpr (I >= 2 && I < 2 * NS + 2) {
+          constexpr int B = (I - 2) % NS * EACH, W = (I - 2) / NS;
+#pragma unroll
+          for (int n = 0; n < EACH; ++n) l += e[I % 2][n], w[W][(B + n) / 8][(B + n) % 8] = (__bf16)e[I % 2][n];
+        }
+        if constexpr (I >= 1 && I < 2 * NS + 1) {
+#pragma unroll
+          for (int n = 0; n < EACH; ++n) e[(I - 1) % 2][n] = __builtin_amdgcn_exp2f(arg[(I - 1) % 2][n]);
+        }
+        if constexpr (I < 2 * NS) {
+#pragma unroll
+          for (int n = 0; n < EACH; ++n) arg[I % 2][n] = fmaf((PART == 0 ? x : y)[N * EACH + n], p.scale_log2, -ref);
+        } else if constexpr (PART == 2) {
+#pragma unroll
+          for (int n = 0; n < EACH; ++n) top = fmaxf(top, z[N * EACH + n]);
+        } else if constexpr (N >= 2) {
+#pragma unroll
+          for (int n = (N - 2) * 16 / (NS - 2); n < (N - 1) * 16 / (NS - 2); ++n) top = fmaxf(top, x[n]);
+        }
+        in_order();
+      });
+      top = half_max(top) * p.scale_log2;
+      asm volatile("" : "+v"(top));
+      __syncthreads();
+    };
     int u = u0;
     while (true) {
       if (moves(top)) move_to(top);
-      // as long as there is nothing out of the ordinary, straight ahead
-      while (!idle && u + 1 < u1 && plain(u) && plain(u + 1)) {
-        bring(u);
-        const float ref = m;
-        bf16x8 w[2][2], rest[2];
-        scores(1 - (u & 1), next);
-        soften(s[0], ref, w[0], rest);
-        soften(s[1], ref, w[1], rest);
-        products(u & 1, 0, w[0]);
-        products(u & 1, 1, w[1]);
-        top = top_of(next[0], next[1]);
-        s[0] = next[0], s[1] = next[1];
+      // as long as there is nothing out of the ordinary, straight ahead, two tiles a turn
+      while (ahead(u)) {
+        straight(u, s[0], s[1], next, std::integral_constant<int, 0>{});
+        s[1] = s[0], s[0] = next;
         ++u;
-        __syncthreads();
         if (moves(top)) break;
       }
       if (moves(top)) move_to(top);
@@ -504,7 +577,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           soften(s[kb], ref, w, rest);
-          if (odd) add_odd(t + 32 * kb);
+          if (__builtin_expect_with_probability(odd, 0, 0.999)) add_odd(t + 32 * kb);
           products(u & 1, kb, w);
         }
         if (u + 1 < u1) {
@@ -727,7 +800,7 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
         else hipLaunchKernelGGL((chunk_kernel<D, WM, WK, KB, KIND, PLACES, false>), grid, dim3(THREADS), 0, st, p);
       };
       if (!a->cache.page_table) go(std::integral_constant<int, kDense>{});
-      else if (a->cache.page_size % C::RPW == 0) go(std::integral_constant<int, kPages>{});
+      else if (a->cache.page_size % C::RPW == 0 && p.c.stride_page < 1ll << 31 && p.c.stride_tok * p.c.page_size < 1ll << 31) go(std::integral_constant<int, kPages>{});
       else go(std::integral_constant<int, kRows>{});
     };
     if (eight) form(std::integral_constant<int, TVA_ROWS_E4M3>{});
