@@ -40,6 +40,7 @@ struct ChunkParams {
   int B, Hq, Hkv, G, W, blocks, max_T;
   int parts, part_keys;  // the most parts a block's tiles are cut into, and the keys of a part that it is cut for
   int window, n_first;   // window: 2^30 where there is none
+  int longest;           // row blocks that are taken from the last on, before the others from the first on
   float scale_log2, v_scale;
 };
 
@@ -142,8 +143,8 @@ __device__ __forceinline__ void times(F f) {
 }
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block (the last ones, which see the
-// most keys, first).
+// Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block: the last ones, which see the
+// most keys, first; where two workgroups per CU hold them all, the second ones from the first on, so that a long and a short one share a CU.
 // PLACES: how a tile's rows are found.  kDense and kPages: the rows that a wave brings at once lie in a sequence, or a page, one after the
 // other: scalar addresses and a lane's offset; kRows: each lane looks for its own (pages that such rows may straddle).
 enum { kDense, kPages, kRows };
@@ -151,7 +152,7 @@ template <int D, int WM, int WK, int KB, int KIND, int PLACES, bool TREE>
 __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams p) {
   typedef ChunkCfg<D, WM, WK, KB, KIND> C;
   __shared__ __align__(16) unsigned char lds[C::LDS];
-  const int g = blockIdx.x, part = blockIdx.y, number = p.blocks - 1 - blockIdx.z;
+  const int g = blockIdx.x, part = blockIdx.y, number = (int)blockIdx.z < p.longest ? p.blocks - 1 - blockIdx.z : blockIdx.z - p.longest;
   const Block k(p, C::R, number);
   const Tiles tiles(p, k, C::KT);
   const int parts = tiles.parts(p, C::KT);
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   // them is no 0), the tile is marked, and rows that see them get them added.  (With remainders every tile: an infinite value times a
   // remainder of 0 or below is no infinity.)
   auto careful_with = [&](int u) __attribute__((always_inline)) { return C::REST || u < quiet0 || u >= quiet1; };
-  auto stash_k = [&](int stage) __attribute__((always_inline)) {
+  auto stash_k = [&](int stage, const u32x4 (&kx)[C::NP]) __attribute__((always_inline)) {
     unsigned char *to = k_stage(stage);
 #pragma unroll
     for (int i = 0; i < C::NP; ++i) {
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       look(u + C::STEP);
       for (; u < u1; u += C::STEP) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        stash_k(wave);
+        stash_k(wave, kx);
         stash_v(u, wave);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         locate(u + C::STEP);
@@ -467,27 +468,30 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     };
     // K of tile u + 2 takes the place of tile u's, V of tile u + 1 that of tile u - 1's
     auto bring = [&](int u) __attribute__((always_inline)) {
-      stash_k(u & 1);
+      stash_k(u & 1, kx);
       stash_v(u + 1, 1 - (u & 1));
       read(vx, p.c.v);  // of tile u + 2
       locate(u + 3);
       read(kx, p.c.k);
       look(u + 4);
     };
-    look(u0);
-    locate(u0);
-    read(kx, p.c.k), read(vx, p.c.v);
-    look(u0 + 1);
-    stash_k(u0 & 1), stash_v(u0, u0 & 1);
-    locate(u0 + 1);
-    look(u0 + 2);
-    read(kx, p.c.k);
-    stash_k(1 - (u0 & 1));
-    read(vx, p.c.v);
-    locate(u0 + 2);
-    look(u0 + 3);
-    read(kx, p.c.k);
-    __syncthreads();
+    {
+      u32x4 k1[C::NP];
+      look(u0);
+      locate(u0);
+      look(u0 + 1);
+      read(kx, p.c.k), read(vx, p.c.v);
+      locate(u0 + 1);
+      look(u0 + 2);
+      read(k1, p.c.k);
+      stash_k(u0 & 1, kx), stash_v(u0, u0 & 1);
+      read(vx, p.c.v);
+      locate(u0 + 2);
+      look(u0 + 3);
+      read(kx, p.c.k);
+      stash_k(1 - (u0 & 1), k1);
+      __syncthreads();
+    }
     float top = -INFINITY;  // of s
     if (!idle) {
       scores(u0 & 1, s);
@@ -507,7 +511,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     //   O with x's   | weights of y
     //   scores x     | largest of z
     //   O with y's   | largest of x
-    constexpr int NS = C::NS, NP = 2 * C::NJ, AHEAD = 4, EACH = 16 / NS;
+    constexpr int NS = C::NS, NP = 2 * C::NJ, AHEAD = WM == 4 ? 3 : 4, EACH = 16 / NS;
     static_assert(NS == NP, "");
     auto straight = [&](int u, f32x16 &x, f32x16 &y, f32x16 &z, auto h) __attribute__((always_inline)) {
       constexpr int H = decltype(h)::value;
@@ -785,6 +789,8 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
   p.parts = pl.parts, p.part_keys = pl.part_keys;
   p.window = a->window ? std::min(a->window, 1 << 30) : 1 << 30, p.n_first = a->window ? a->n_first : 0;
   p.scale_log2 = a->scale * kLog2e * k_scale, p.v_scale = !eight || a->cache.v_scale == 0.f ? 1.f : a->cache.v_scale;
+  const int first_round = 256 / a->Hkv;
+  p.longest = pl.rows == 128 && pl.parts == 1 && pl.blocks > first_round && pl.blocks <= 2 * first_round ? first_round : pl.blocks;
   const dim3 grid(a->Hkv, pl.parts, pl.blocks);
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();

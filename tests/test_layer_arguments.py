@@ -120,7 +120,7 @@ def status(which, **fields):
     ("append", dict(r__k=None, r__k_out=None), -1), ("append", dict(v=None), -1), ("append", dict(v=8), -1), ("append", dict(v_stride=4), -1), ("append", dict(r__L=None), -1),
     ("append", dict(cache__kind=3), -1), ("append", dict(cache__kind=2), -1), ("append", dict(cache__cu_L=None), -1), ("append", dict(cache__stride_tok=4), -1), ("append", dict(r__dims=8), -2),
     ("attn", dict(B=0), -1), ("attn", dict(Hkv=3), -1), ("attn", dict(D=32), -2), ("attn", dict(scale=0.0), -1), ("attn", dict(window=-1), -1), ("attn", dict(n_first=-1), -1),
-    ("attn", dict(num_splits=-1), -1), ("attn", dict(plan_rows=48), -1), ("attn", dict(max_T=129), -2), ("attn", dict(mask_words=0), -2), ("attn", dict(cache__kind=2), -2),
+    ("attn", dict(num_splits=-1), -1), ("attn", dict(plan_rows=64), -1), ("attn", dict(max_T=129), -2), ("attn", dict(mask_words=0), -2), ("attn", dict(cache__kind=2), -2),
     ("attn", dict(cache__kind=9), -1), ("attn", dict(q_stride=8), -1), ("attn", dict(q_stride=HQ * D + 4), -1), ("attn", dict(q=None), -1), ("attn", dict(out=None), -1),
     ("attn", dict(L=None), -1), ("attn", dict(q=8), -1), ("attn", dict(max_L=1 << 30), -2), ("attn", dict(anc_mask=None, max_T=1 << 29), -2), ("attn", dict(workspace=8, workspace_bytes=1 << 30, num_splits=2, max_L=4000), -1),
     ("attn", dict(workspace_bytes=4, num_splits=2, workspace=64, max_L=4000), -3), ("attn", dict(cache__page_table=64), -1), ("attn", dict(cache__v=None), -1),
