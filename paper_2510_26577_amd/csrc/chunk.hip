@@ -85,8 +85,9 @@ struct Tiles {
   }
   __device__ __forceinline__ int at(int u) const { return u < first ? u : u - first + main; }
   __device__ __forceinline__ int parts(const ChunkParams &p, int KT) const {
-    const int tiles = max(1, p.part_keys / KT);
-    return same(max(1, min(p.parts, (n + tiles - 1) / tiles)));
+    if (p.parts == 1) return 1;
+    const uint32_t tiles = max(1, p.part_keys / KT);
+    return same(max(1, min(p.parts, (int)((n + tiles - 1) / tiles))));
   }
 };
 
@@ -94,13 +95,14 @@ __device__ __forceinline__ float half_max(float x) {
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-// whether any of eight bf16 numbers is infinite or NaN
-__device__ __forceinline__ bool not_finite(u32x4 x) {
-  bool any = false;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+// The larger, of each half, of |x| bits and those of eight bf16 numbers; and whether one of them is infinite or NaN
+__device__ __forceinline__ u16x2 larger(u32x4 v, u16x2 x) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) any |= (x[k] & 0x7f80) == 0x7f80 || (x[k] & 0x7f800000) == 0x7f800000;
-  return any;
+  for (int k = 0; k < 4; ++k) x = __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, v[k] & 0x7fff7fffu));
+  return x;
 }
+__device__ __forceinline__ bool not_finite(u16x2 x) { return max(x[0], x[1]) >= 0x7f80; }
 __device__ __forceinline__ u32x4 finite_ones(u32x4 x) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -157,7 +159,9 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   const Tiles tiles(p, k, C::KT);
   const int parts = tiles.parts(p, C::KT);
   if (k.rows <= 0 || part >= parts) return;
-  const int u0 = same((int)((int64_t)tiles.n * part / parts)), u1 = same((int)((int64_t)tiles.n * (part + 1) / parts));
+  // (parts differ by a tile at most: the first n % parts have one more)
+  const int each = parts == 1 ? tiles.n : (int)((uint32_t)tiles.n / (uint32_t)parts), more = tiles.n - each * parts;
+  const int u0 = same(part * each + min(part, more)), u1 = same(u0 + each + (part < more));
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wm = wave % WM, wk = wave / WM;
@@ -308,20 +312,28 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     unsigned char *to = v_stage(stage);
     const bool careful = careful_with(u);
     bool odd = false;
+    constexpr int PER = KIND == TVA_ROWS_BF16 ? 1 : C::EPL / 8;
+    u32x4 v[C::NP * PER];
 #pragma unroll
-    for (int i = 0; i < C::NP; ++i) {
-      const int r = (i * C::TOGETHER + bring) * C::RPW + lrow;
-#pragma unroll
-      for (int h = 0; h < (KIND == TVA_ROWS_BF16 ? 1 : C::EPL / 8); ++h) {
-        u32x4 v = vx[i];
-        if constexpr (KIND != TVA_ROWS_BF16) v = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i][2 * h], vx[i][2 * h + 1]}));
-        if (careful && not_finite(v)) odd = true, v = finite_ones(v);
-        *(u32x4 *)(to + r * C::V_ROW + (C::EPL / 8 * piece + h) * 16) = v;
-      }
+    for (int i = 0; i < C::NP * PER; ++i) {
+      v[i] = vx[i / PER];
+      if constexpr (KIND != TVA_ROWS_BF16) v[i] = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i / PER][i % PER * 2], vx[i / PER][i % PER * 2 + 1]}));
     }
     if (careful) {
-      const bool any = __any(odd);
-      if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = any;
+      u16x2 x = {0, 0};
+#pragma unroll
+      for (int i = 0; i < C::NP * PER; ++i) x = larger(v[i], x);
+      odd = __any(not_finite(x));
+      if (__builtin_expect_with_probability(odd, 0, 0.999)) {
+#pragma unroll
+        for (int i = 0; i < C::NP * PER; ++i) v[i] = finite_ones(v[i]);
+      }
+      if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = odd;
+    }
+#pragma unroll
+    for (int i = 0; i < C::NP * PER; ++i) {
+      const int r = (i / PER * C::TOGETHER + bring) * C::RPW + lrow;
+      *(u32x4 *)(to + r * C::V_ROW + (PER * piece + i % PER) * 16) = v[i];
     }
   };
   auto is_odd = [&](int u, int stage) __attribute__((always_inline)) -> bool {
@@ -599,13 +611,30 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   // ---- the key groups' results joined, and O^T turned over to rows ----
   l = half_sum(l);
   __syncthreads();
-  float *patch = (float *)lds, *maxima = (float *)(lds + C::WAVES * C::PATCH), *sums = maxima + C::WAVES * 32;
-  if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
-  __syncthreads();
-  float top = -INFINITY;
+  float *patch = (float *)lds + wave * (32 * C::TP), *maxima = (float *)(lds + C::WAVES * C::PATCH), *sums = maxima + C::WAVES * 32;
+  float top = m, sum = l;
+  if constexpr (WK > 1) {
+    if (half == 0) maxima[wave * 32 + l32] = m, sums[wave * 32 + l32] = l;
+    __syncthreads();
 #pragma unroll
-  for (int x = 0; x < WK; ++x) top = fmaxf(top, maxima[(x * WM + wm) * 32 + l32]);
-  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    for (int x = 0; x < WK; ++x) top = fmaxf(top, maxima[(x * WM + wm) * 32 + l32]);
+    sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < WK; ++x) {
+      const float mx = maxima[(x * WM + wm) * 32 + l32], lx = sums[(x * WM + wm) * 32 + l32];
+      sum += mx == -INFINITY ? lx : lx * __builtin_amdgcn_exp2f(mx - top);  // (0, or NaN)
+    }
+  }
+  // what a row's O is multiplied by (NaN stays NaN), and where it goes
+  const float f = (sum == 0.f ? 0.f : p.v_scale / sum) * (WK == 1 ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top));
+  const bool whole = parts == 1;
+  const int64_t slot0 = (((int64_t)number * p.parts + part) * p.Hkv + g) * C::R;
+  const int64_t to = whole ? (int64_t)(k.t0 + node) * p.Hq + head : slot0 + wm * 32 + l32;
+  if (wk == 0 && half == 0 && wm * 32 + l32 < k.rows) {
+    const float lse = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
+    if (!whole) p.part_lse[to] = lse;
+    else if (p.lse) p.lse[to] = lse;
+  }
 #pragma unroll
   for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
@@ -613,37 +642,37 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       f32x4 x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = acc[j][i * 4 + e] * f;
-      *(f32x4 *)(patch + wave * (32 * C::TP) + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
+      *(f32x4 *)(patch + l32 * C::TP + j * 32 + 8 * i + 4 * half) = x;
     }
-  __syncthreads();
-  const int64_t slot0 = (((int64_t)number * p.parts + part) * p.Hkv + g) * C::R;
-  for (int x = tid; x < C::R * (D / 4); x += C::THREADS) {
-    const int r = x / (D / 4), d = (x - r * (D / 4)) * 4, w = r >> 5, rr = r & 31;
-    if (r >= k.rows) break;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float top_r = -INFINITY, sum = 0.f;
+  if constexpr (WK > 1) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // a wave's rows are those of its row group; with several key groups each takes its share of them
+  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, ROUNDS = 32 / WK / AT_ONCE, U = 4;
+  const int d = lane % LANES * 4;
+#pragma unroll 1
+  for (int n = 0; n < ROUNDS; n += U) {
+    f32x4 o[U];
+    int64_t at[U];
 #pragma unroll
-    for (int y = 0; y < WK; ++y) top_r = fmaxf(top_r, maxima[(y * WM + w) * 32 + rr]);
+    for (int u = 0; u < U; ++u) {
+      const int r = wk * (32 / WK) + (n + u) * AT_ONCE + lane / LANES;
+      o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int y = 0; y < WK; ++y) {
-      const int at = y * WM + w;
-      o += *(const f32x4 *)(patch + at * (32 * C::TP) + rr * C::TP + d);
-      const float my = maxima[at * 32 + rr];
-      sum += my == -INFINITY ? sums[at * 32 + rr] : sums[at * 32 + rr] * __builtin_amdgcn_exp2f(my - top_r);  // (0, or NaN)
+      for (int x = 0; x < WK; ++x) o[u] += *(const f32x4 *)((const float *)lds + (x * WM + wm) * (32 * C::TP) + r * C::TP + d);
+      at[u] = __shfl(to, r);
+      if (wm * 32 + r >= k.rows) at[u] = -1;
     }
-    o *= sum == 0.f ? 0.f : p.v_scale / sum;  // (NaN stays NaN)
-    const float lse = sum == 0.f ? -INFINITY : (top_r + __builtin_amdgcn_logf(sum)) * kLn2;  // (logf: base 2)
-    if (parts == 1) {
-      const int rnode = (k.row0 + r) / p.G, rhead = g * p.G + (k.row0 + r - rnode * p.G);
-      const int64_t at = (int64_t)(k.t0 + rnode) * p.Hq + rhead;
-      bf16x4 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = (__bf16)o[e];
-      *(bf16x4 *)(p.out + at * D + d) = y;
-      if (d == 0 && p.lse) p.lse[at] = lse;
-    } else {
-      *(f32x4 *)(p.part_out + (slot0 + r) * D + d) = o;
-      if (d == 0) p.part_lse[slot0 + r] = lse;
+    for (int u = 0; u < U; ++u) {
+      if (at[u] < 0) continue;
+      if (whole) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)o[u][e];
+        *(bf16x4 *)(p.out + at[u] * D + d) = y;
+      } else {
+        *(f32x4 *)(p.part_out + at[u] * D + d) = o[u];
+      }
     }
   }
 }
