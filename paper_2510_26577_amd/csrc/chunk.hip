@@ -308,9 +308,8 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       }
     }
   };
-  auto stash_v = [&](int u, int stage) __attribute__((always_inline)) {
+  auto stash_v = [&](bool careful, int stage) __attribute__((always_inline)) {
     unsigned char *to = v_stage(stage);
-    const bool careful = careful_with(u);
     bool odd = false;
     constexpr int PER = KIND == TVA_ROWS_BF16 ? 1 : C::EPL / 8;
     u32x4 v[C::NP * PER];
@@ -432,7 +431,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       for (; u < u1; u += C::STEP) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         stash_k(wave, kx);
-        stash_v(u, wave);
+        stash_v(careful_with(u), wave);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         locate(u + C::STEP);
         read(kx, p.c.k), read(vx, p.c.v);
@@ -481,7 +480,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     // K of tile u + 2 takes the place of tile u's, V of tile u + 1 that of tile u - 1's
     auto bring = [&](int u) __attribute__((always_inline)) {
       stash_k(u & 1, kx);
-      stash_v(u + 1, 1 - (u & 1));
+      stash_v(careful_with(u + 1), 1 - (u & 1));
       read(vx, p.c.v);  // of tile u + 2
       locate(u + 3);
       read(kx, p.c.k);
@@ -496,7 +495,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       locate(u0 + 1);
       look(u0 + 2);
       read(k1, p.c.k);
-      stash_k(u0 & 1, kx), stash_v(u0, u0 & 1);
+      stash_k(u0 & 1, kx), stash_v(careful_with(u0), u0 & 1);
       read(vx, p.c.v);
       locate(u0 + 2);
       look(u0 + 3);
@@ -527,7 +526,6 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     static_assert(NS == NP, "");
     auto straight = [&](int u, f32x16 &x, f32x16 &y, f32x16 &z, auto h) __attribute__((always_inline)) {
       constexpr int H = decltype(h)::value;
-      bring(u);
       const float ref = m;
       const unsigned char *kt = k_stage(1 - (u & 1)), *vt = v_stage(u & 1);
       bf16x8 ops[AHEAD], w[2][2];
@@ -547,6 +545,12 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
         else if constexpr (PART == 2) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, q[N], N == 0 ? f32x16{} : x, 0, 0, 0);
         else acc[N % C::NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, w[PART / 2][N / C::NJ], acc[N % C::NJ], 0, 0, 0);
         fetch(std::integral_constant<int, I + AHEAD>{});
+        // what bring() does, a step at a time
+        if constexpr (I == 1) stash_k(u & 1, kx);
+        if constexpr (I == 3) stash_v(false, 1 - (u & 1));
+        if constexpr (I == 5) read(vx, p.c.v), locate(u + 3);
+        if constexpr (I == 6) read(kx, p.c.k);
+        if constexpr (I == 7) look(u + 4);
         // arguments of turn I, exponentials of turn I - 1, sums and roundings of turn I - 2 (a half's last ones are done in the next part's first turns)
         if constexpr (I >= 2 && I < 2 * NS + 2) {
           constexpr int B = (I - 2) % NS * EACH, W = (I - 2) / NS;
@@ -563,13 +567,14 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
         } else if constexpr (PART == 2) {
 #pragma unroll
           for (int n = 0; n < EACH; ++n) top = fmaxf(top, z[N * EACH + n]);
-        } else if constexpr (N >= 2) {
+        } else if constexpr (N >= NS / 4 && N < NS - 1) {  // (the last product is some turns old)
+          constexpr int TURNS = NS - 1 - NS / 4, TURN = N - NS / 4;
 #pragma unroll
-          for (int n = (N - 2) * 16 / (NS - 2); n < (N - 1) * 16 / (NS - 2); ++n) top = fmaxf(top, x[n]);
+          for (int n = TURN * 16 / TURNS; n < (TURN + 1) * 16 / TURNS; ++n) top = fmaxf(top, x[n]);
         }
+        if constexpr (I == 4 * NS - 1) top = half_max(top) * p.scale_log2;
         in_order();
       });
-      top = half_max(top) * p.scale_log2;
       asm volatile("" : "+v"(top));
       __syncthreads();
     };
