@@ -128,6 +128,7 @@ struct ChunkCfg {
   static constexpr int TOGETHER = OWN ? 1 : WAVES;                        // waves that bring a tile
   static constexpr int EPL = KIND == TVA_ROWS_BF16 || KT * D / 16 < 64 * TOGETHER ? 8 : 16;  // elements that a lane brings at once
   static constexpr int LPR = D / EPL, RPW = 64 / LPR;                     // lanes that bring a row, rows that a wave brings at once
+  static constexpr int PIECES = EPL / 8;                                   // 16-byte pieces of bf16 that they become
   static constexpr int NP = KT / (RPW * TOGETHER);                        // reads per lane and tile (of K, and of V)
   static_assert(KT % (RPW * TOGETHER) == 0, "");
   static constexpr int TP = D + 4, PATCH = 32 * TP * 4;  // an output patch per wave, floats between its rows
@@ -169,7 +170,6 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   // ---- this lane's query row (column of S^T and O^T); rows past the end repeat the last one and are not written ----
   const int row = k.row0 + min(wm * 32 + l32, k.rows - 1);
   const int node = row / p.G, head = g * p.G + (row - node * p.G);
-  const bool idle = wm * 32 >= k.rows;
   bf16x8 q[C::NS];
   {
     const __bf16 *from = p.q + (int64_t)(k.t0 + node) * p.q_stride + head * D + half * 8;
@@ -308,32 +308,33 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       }
     }
   };
-  auto stash_v = [&](bool careful, int stage) __attribute__((always_inline)) {
+  auto stash_v = [&](int stage) __attribute__((always_inline)) {
     unsigned char *to = v_stage(stage);
-    bool odd = false;
-    constexpr int PER = KIND == TVA_ROWS_BF16 ? 1 : C::EPL / 8;
-    u32x4 v[C::NP * PER];
 #pragma unroll
-    for (int i = 0; i < C::NP * PER; ++i) {
-      v[i] = vx[i / PER];
-      if constexpr (KIND != TVA_ROWS_BF16) v[i] = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i / PER][i % PER * 2], vx[i / PER][i % PER * 2 + 1]}));
-    }
-    if (careful) {
-      u16x2 x = {0, 0};
+    for (int i = 0; i < C::NP; ++i) {
+      const int r = (i * C::TOGETHER + bring) * C::RPW + lrow;
 #pragma unroll
-      for (int i = 0; i < C::NP * PER; ++i) x = larger(v[i], x);
-      odd = __any(not_finite(x));
-      if (__builtin_expect_with_probability(odd, 0, 0.999)) {
-#pragma unroll
-        for (int i = 0; i < C::NP * PER; ++i) v[i] = finite_ones(v[i]);
+      for (int h = 0; h < C::PIECES; ++h) {
+        u32x4 v = vx[i];
+        if constexpr (KIND != TVA_ROWS_BF16) v = __builtin_bit_cast(u32x4, widen8_e4m3(u32x2{vx[i][2 * h], vx[i][2 * h + 1]}));
+        *(u32x4 *)(to + r * C::V_ROW + (C::PIECES * piece + h) * 16) = v;
       }
-      if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = odd;
     }
+  };
+  auto look_through = [&](int stage) __attribute__((always_inline)) {  // at what this lane has brought
+    unsigned char *to = v_stage(stage);
+    u16x2 x = {0, 0};
 #pragma unroll
-    for (int i = 0; i < C::NP * PER; ++i) {
-      const int r = (i / PER * C::TOGETHER + bring) * C::RPW + lrow;
-      *(u32x4 *)(to + r * C::V_ROW + (PER * piece + i % PER) * 16) = v[i];
+    for (int i = 0; i < C::NP * C::PIECES; ++i)
+      x = larger(*(const u32x4 *)(to + ((i / C::PIECES * C::TOGETHER + bring) * C::RPW + lrow) * C::V_ROW + (C::PIECES * piece + i % C::PIECES) * 16), x);
+    const bool odd = __any(not_finite(x));
+    if (odd) {
+      for (int i = 0; i < C::NP * C::PIECES; ++i) {
+        u32x4 *v = (u32x4 *)(to + ((i / C::PIECES * C::TOGETHER + bring) * C::RPW + lrow) * C::V_ROW + (C::PIECES * piece + i % C::PIECES) * 16);
+        *v = finite_ones(*v);
+      }
     }
+    if (lane == 0) ((int *)(lds + C::ODD))[(C::OWN ? 0 : stage * C::WAVES) + wave] = odd;
   };
   auto is_odd = [&](int u, int stage) __attribute__((always_inline)) -> bool {
     bool odd = false;
@@ -431,7 +432,8 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       for (; u < u1; u += C::STEP) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         stash_k(wave, kx);
-        stash_v(careful_with(u), wave);
+        stash_v(wave);
+        if (careful_with(u)) look_through(wave);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         locate(u + C::STEP);
         read(kx, p.c.k), read(vx, p.c.v);
@@ -462,30 +464,6 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     // Beside the softmax of tile u run the products of tile u + 1's scores, beside those of O with tile u the search for tile u + 1's largest
     // scores: matrix and vector instructions of a wave that do not wait for each other.  K's tiles are therefore a tile ahead of V's.
     f32x16 s[2], next;
-    auto scores = [&](int stage, f32x16 (&s)[2]) __attribute__((always_inline)) {
-      const unsigned char *kt = k_stage(stage);
-      s[0] = f32x16{}, s[1] = f32x16{};
-#pragma unroll
-      for (int st = 0; st < C::NS; ++st)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(kt, kb, st), q[st], s[kb], 0, 0, 0);
-    };
-    auto products = [&](int stage, int kb, const bf16x8 (&w)[2]) __attribute__((always_inline)) {
-      const unsigned char *vt = v_stage(stage);
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int j = 0; j < C::NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vt, kb, a, j), w[a], acc[j], 0, 0, 0);
-    };
-    // K of tile u + 2 takes the place of tile u's, V of tile u + 1 that of tile u - 1's
-    auto bring = [&](int u) __attribute__((always_inline)) {
-      stash_k(u & 1, kx);
-      stash_v(careful_with(u + 1), 1 - (u & 1));
-      read(vx, p.c.v);  // of tile u + 2
-      locate(u + 3);
-      read(kx, p.c.k);
-      look(u + 4);
-    };
     {
       u32x4 k1[C::NP];
       look(u0);
@@ -495,7 +473,8 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       locate(u0 + 1);
       look(u0 + 2);
       read(k1, p.c.k);
-      stash_k(u0 & 1, kx), stash_v(careful_with(u0), u0 & 1);
+      stash_k(u0 & 1, kx), stash_v(u0 & 1);
+      if (careful_with(u0)) look_through(u0 & 1);
       read(vx, p.c.v);
       locate(u0 + 2);
       look(u0 + 3);
@@ -503,17 +482,18 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
       stash_k(1 - (u0 & 1), k1);
       __syncthreads();
     }
-    float top = -INFINITY;  // of s
-    if (!idle) {
-      scores(u0 & 1, s);
-      const int t = tiles.at(u0) * C::KT;
-      if (!all_seen(t, C::KT, low, high)) mask(s[0], t), mask(s[1], t + 32);
-      top = top_of(s[0], s[1]);
+    {
+      const unsigned char *kt = k_stage(u0 & 1);
+      s[0] = f32x16{}, s[1] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < C::NS; ++st)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(kt, kb, st), q[st], s[kb], 0, 0, 0);
     }
-    __syncthreads();  // (K's first tile has been read)
-    // tiles without marks, the next one too and seen by all rows of the wave: tile u of those below `until`
-    const int from = max(quiet0, plain0), until = idle ? 0 : min(min(quiet1, plain1), u1) - 1;
-    auto ahead = [&](int u) __attribute__((always_inline)) { return u >= from && u < until; };
+    const int t = tiles.at(u0) * C::KT;
+    if (!all_seen(t, C::KT, low, high)) mask(s[0], t), mask(s[1], t + 32);
+    float top = top_of(s[0], s[1]);  // of s
+    __syncthreads();                 // (K's first tile has been read)
     // A tile in the order in which it runs (left to itself the compiler has all products first and their operands' reads right before them):
     // per matrix instruction the softmax of EACH scores, in three steps of which each waits for none of its own turn, and an operand read AHEAD
     // matrix instructions ahead.  x holds the scores of half h of tile u, y those of the other; z takes those of half h of tile u + 1, then x
@@ -524,15 +504,14 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
     //   O with y's   | largest of x
     constexpr int NS = C::NS, NP = 2 * C::NJ, AHEAD = WM == 4 ? 3 : 4, EACH = 16 / NS;
     static_assert(NS == NP, "");
-    auto straight = [&](int u, f32x16 &x, f32x16 &y, f32x16 &z, auto h) __attribute__((always_inline)) {
-      constexpr int H = decltype(h)::value;
-      const float ref = m;
+    auto straight = [&](int u, f32x16 &x, f32x16 &y, f32x16 &z) __attribute__((always_inline)) {
+      const float ref = m == -INFINITY ? 0.f : m;
       const unsigned char *kt = k_stage(1 - (u & 1)), *vt = v_stage(u & 1);
       bf16x8 ops[AHEAD], w[2][2];
       float arg[2][EACH], e[2][EACH];
       top = -INFINITY;
       auto fetch = [&](auto i) __attribute__((always_inline)) {  // of matrix instruction i
-        constexpr int I = decltype(i)::value, PART = I / NS, N = I % NS, HALF = PART < 2 ? H : 1 - H;
+        constexpr int I = decltype(i)::value, PART = I / NS, N = I % NS, HALF = PART / 2;
         if constexpr (PART == 0 || PART == 2) ops[I % AHEAD] = k_operand(kt, HALF, N);
         else if constexpr (PART < 4) ops[I % AHEAD] = v_operand(vt, HALF, N / C::NJ, N % C::NJ);
       };
@@ -545,9 +524,9 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
         else if constexpr (PART == 2) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, q[N], N == 0 ? f32x16{} : x, 0, 0, 0);
         else acc[N % C::NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, w[PART / 2][N / C::NJ], acc[N % C::NJ], 0, 0, 0);
         fetch(std::integral_constant<int, I + AHEAD>{});
-        // what bring() does, a step at a time
+        // K of tile u + 2 takes the place of tile u's, V of tile u + 1 that of tile u - 1's; the next ones are asked for
         if constexpr (I == 1) stash_k(u & 1, kx);
-        if constexpr (I == 3) stash_v(false, 1 - (u & 1));
+        if constexpr (I == 3) stash_v(1 - (u & 1));
         if constexpr (I == 5) read(vx, p.c.v), locate(u + 3);
         if constexpr (I == 6) read(kx, p.c.k);
         if constexpr (I == 7) look(u + 4);
@@ -576,39 +555,22 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
         in_order();
       });
       asm volatile("" : "+v"(top));
-      __syncthreads();
     };
-    int u = u0;
-    while (true) {
+    // behind tile u with ahead0 <= u < ahead1 there is nothing to look at
+    const int ahead0 = max(quiet0, plain0) - 1, ahead1 = min(min(quiet1, plain1), u1) - 1;
+    for (int u = u0; u < u1; ++u) {
       if (moves(top)) move_to(top);
-      // as long as there is nothing out of the ordinary, straight ahead, two tiles a turn
-      while (ahead(u)) {
-        straight(u, s[0], s[1], next, std::integral_constant<int, 0>{});
-        s[1] = s[0], s[0] = next;
-        ++u;
-        if (moves(top)) break;
-      }
-      if (moves(top)) move_to(top);
-      if (u + 1 < u1) bring(u);
-      if (!idle) {
-        const float ref = m == -INFINITY ? 0.f : m;
-        const int t = tiles.at(u) * C::KT;
-        const bool odd = is_odd(u, u & 1);
-        bf16x8 w[2], rest[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          soften(s[kb], ref, w, rest);
-          if (__builtin_expect_with_probability(odd, 0, 0.999)) add_odd(t + 32 * kb);
-          products(u & 1, kb, w);
-        }
-        if (u + 1 < u1) {
-          scores(1 - (u & 1), s);
-          const int t = tiles.at(u + 1) * C::KT;
-          if (!all_seen(t, C::KT, low, high)) mask(s[0], t), mask(s[1], t + 32);
+      if (is_odd(u, u & 1)) add_odd(tiles.at(u) * C::KT), add_odd(tiles.at(u) * C::KT + 32);
+      straight(u, s[0], s[1], next);  // (behind the last tile: its scores again, which nobody takes)
+      s[1] = s[0], s[0] = next;
+      if (u < ahead0 || u >= ahead1) {
+        if (careful_with(u + 1)) look_through(1 - (u & 1));
+        const int t = first_slot(u + 1);
+        if (!all_seen(t, C::KT, low, high)) {
+          mask(s[0], t), mask(s[1], t + 32);
           top = top_of(s[0], s[1]);
         }
       }
-      if (++u >= u1) break;
       __syncthreads();
     }
   }
