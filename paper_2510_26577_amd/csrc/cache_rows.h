@@ -103,6 +103,22 @@ __device__ __forceinline__ float half_sum(float x) {
 
 __device__ __forceinline__ float exponent_byte(uint32_t x) { return __uint_as_float(x << 23); }  // 2^(x - 127), x of 1 .. 254
 
+// What 4, 8 or 16 neighbouring lanes hold, added up or the largest of it, in each of them: lanes exchanged inside the vector instructions
+// (by shuffles through LDS each step waits for its answer)
+template <int CTRL, class T>
+__device__ __forceinline__ T exchanged(T x) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int N, class T, class F>
+__device__ __forceinline__ T over_lanes(T x, F f) {
+  static_assert(N == 4 || N == 8 || N == 16, "");
+  x = f(x, exchanged<0xb1>(x));                        // lanes 1, 0, 3, 2
+  x = f(x, exchanged<0x4e>(x));                        // lanes 2, 3, 0, 1
+  if constexpr (N >= 8) x = f(x, exchanged<0x141>(x));  // eight lanes the other way round
+  if constexpr (N >= 16) x = f(x, exchanged<0x140>(x)); // sixteen
+  return x;
+}
+
 // |x| bits of the largest finite of eight bf16 numbers, and whether all are finite
 __device__ __forceinline__ uint32_t largest(const u16x8 x, bool *finite) {
   uint32_t a = 0, all = 0;
@@ -163,8 +179,7 @@ template <int LPR>
 __device__ __forceinline__ uint32_t round_k(const u16x8 k, uint32_t *scale) {
   bool fine;
   uint32_t a = largest(k, &fine);
-#pragma unroll
-  for (int o = 1; o < 4; o *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+  a = over_lanes<4>(a, [](uint32_t x, uint32_t y) { return max(x, y); });
   const int e = (int)(a >> 7) - 127 - ((a & 127) > 64 ? 1 : 2), kept = min(max(e, -96), 124);
   const float s = exponent_byte((uint32_t)(kept + 127));
   uint32_t w = codes_k(k, s);
@@ -177,8 +192,7 @@ template <int LPR>
 __device__ __forceinline__ uint32_t round_v(const u16x8 v, float *scale) {
   bool fine;
   uint32_t a = largest(v, &fine);
-#pragma unroll
-  for (int o = 1; o < LPR; o *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+  a = over_lanes<LPR>(a, [](uint32_t x, uint32_t y) { return max(x, y); });
   const int n = 128 + (int)(a & 127), e = (int)(a >> 7) - 126;
   const float s = fminf(fmaxf(n < 192 ? ldexpf((float)((n + 11) / 12), e - 7) : ldexpf((float)((n + 23) / 24), e - 6), 0x1p-96f), 0x1p124f);
   uint32_t w = codes_v(v, s);

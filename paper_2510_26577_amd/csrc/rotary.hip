@@ -86,8 +86,8 @@ __device__ __forceinline__ void to_cache(const CacheView &c, bool is_v, int64_t 
 
 constexpr int kNoCache = -1;
 
-// KIND: of the cache's rows, or kNoCache
-template <int D, bool INTERLEAVED, int KIND>
+// KIND: of the cache's rows, or kNoCache.  NORM: q's or k's heads are normed
+template <int D, bool INTERLEAVED, int KIND, bool NORM>
 __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams p) {
   constexpr int LPR = D / 8, HEADS = 64 / LPR, U = kRowsInFlight;
   __shared__ float2 turns[kWaves][D / 2];
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
   const int other = INTERLEAVED || !turned ? piece : piece < half ? piece + half : piece - half;
 
   // ---- the rows (all reads come before the first write: the outputs may be the inputs) ----
-  u16x8 x[U], y[U];
+  u16x8 x[U];
   int head[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -114,11 +114,13 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
     head[u] = (is_q ? at : is_k ? at - p.q_pieces : at - p.q_pieces - p.k_pieces) * HEADS + lane / LPR;
     const char *from = is_q ? p.q + row * p.q_stride * 2 : is_k ? p.k + row * p.k_stride * 2 : p.v + row * p.v_stride * 2;
     from += min(head[u], H - 1) * (D * 2);
-    if (at < p.q_pieces + p.k_pieces + p.v_pieces) {
-      x[u] = *(const u16x8 *)(from + piece * 16);
-      if (!INTERLEAVED && at < p.q_pieces + p.k_pieces) y[u] = *(const u16x8 *)(from + other * 16);
-    }
+    if (at < p.q_pieces + p.k_pieces + p.v_pieces) x[u] = *(const u16x8 *)(from + piece * 16);
   }
+
+  // the weights of the first heads' norm
+  const uint16_t *norm = !NORM ? nullptr : first < p.q_pieces ? p.q_norm : p.k_norm;
+  u16x8 w = {}, wz = {};
+  if (NORM && norm) w = *(const u16x8 *)(norm + piece * 8), wz = *(const u16x8 *)(norm + other * 8);
 
   // ---- the token's place and position ----
   int b = 0, i = (int)row, P = 0, start = 0;
@@ -144,17 +146,21 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
     turns[wave][lane] = make_float2(c * p.magnitude, s * p.magnitude);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  // this lane's element e becomes x[e] * own[e] + its pair's other element * with[e]
+  // this lane's element e becomes x[e] * own[e] + its pair's other element * with[e], a norm's weights taken in
   float own[8], with[8];
+  auto turn = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    own[e] = 1.f, with[e] = 0.f;
-    if (turned) {
-      const bool second = INTERLEAVED ? e % 2 : piece >= half;
-      const float2 t = turns[wave][INTERLEAVED ? piece * 4 + e / 2 : (second ? piece - half : piece) * 8 + e];
-      own[e] = t.x, with[e] = second ? t.y : -t.y;
+    for (int e = 0; e < 8; ++e) {
+      own[e] = 1.f, with[e] = 0.f;
+      if (turned) {
+        const bool second = INTERLEAVED ? e % 2 : piece >= half;
+        const float2 t = turns[wave][INTERLEAVED ? piece * 4 + e / 2 : (second ? piece - half : piece) * 8 + e];
+        own[e] = t.x, with[e] = second ? t.y : -t.y;
+      }
+      if (NORM && norm) own[e] *= widen(w[e]), with[e] *= widen(INTERLEAVED ? w[e ^ 1] : wz[e]);
     }
-  }
+  };
+  turn();
   bool room = false;
   int64_t at_cache = 0;
   if constexpr (KIND != kNoCache) {
@@ -176,32 +182,33 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
         if (room) to_cache<D, KIND>(p.c, true, at_cache + head[u] * p.c.stride_head, piece, x[u], p.v_scale, valid);
       continue;
     }
-    float a[8], z[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      a[e] = widen(x[u][e]);
-      z[e] = INTERLEAVED ? widen(x[u][e ^ 1]) : widen(y[u][e]);
+    if (NORM && u > 0 && at == p.q_pieces) {  // k's heads have a norm of their own
+      norm = p.k_norm;
+      if (norm) w = *(const u16x8 *)(norm + piece * 8), wz = *(const u16x8 *)(norm + other * 8);
+      turn();
     }
-    const uint16_t *norm = is_q ? p.q_norm : p.k_norm;
-    if (norm) {
+    u16x8 y = x[u];
+    if constexpr (!INTERLEAVED) {
+      u32x4 from = __builtin_bit_cast(u32x4, x[u]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) from[e] = (uint32_t)__builtin_amdgcn_ds_bpermute((lane - piece + other) * 4, (int)from[e]);
+      y = __builtin_bit_cast(u16x8, from);
+    }
+    float f = 1.f;
+    if (NORM && norm) {
       float s = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(a[e], a[e], s);
-#pragma unroll
-      for (int o = 1; o < LPR; o *= 2) s += __shfl_xor(s, o);
-      const float f = 1.f / sqrtf(s * (1.f / D) + p.eps);
-      const u16x8 w = *(const u16x8 *)(norm + piece * 8), wz = *(const u16x8 *)(norm + other * 8);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        a[e] = a[e] * f * widen(w[e]);
-        z[e] = z[e] * f * widen(INTERLEAVED ? w[e ^ 1] : wz[e]);
-      }
+      for (int e = 0; e < 8; ++e) s = fmaf(widen(x[u][e]), widen(x[u][e]), s);
+      s = over_lanes<LPR>(s, [](float x, float y) { return x + y; });
+      f = 1.f / sqrtf(s * (1.f / D) + p.eps);
     }
     u16x8 out;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      // (elements that are not turned are not mixed with others either: 0 * inf)
-      out[e] = narrow(turned ? fmaf(a[e], own[e], z[e] * with[e]) : a[e]);
+      const float a = widen(x[u][e]), z = widen(y[INTERLEAVED ? e ^ 1 : e]);
+      float r = a * own[e];
+      if (turned) r = fmaf(z, with[e], r);  // (elements that are not turned are not mixed with others either: 0 * inf)
+      out[e] = narrow(NORM ? r * f : r);
     }
     if (is_q) {
       if (valid) *(u16x8 *)(p.q_out + (row * p.q_out_stride + head[u] * D + piece * 8) * 2) = out;
@@ -254,7 +261,10 @@ int launch(const tva_rotate_args *a, RotateParams &p, hipStream_t st) {
   if (blocks > 0x7fffffff) return TVA_UNSUPPORTED;
   (void)hipGetLastError();
   auto go = [&](auto d, auto inter) {
-    hipLaunchKernelGGL((rotate_kernel<decltype(d)::value, decltype(inter)::value, KIND>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, st, p);
+    constexpr int D = decltype(d)::value;
+    constexpr bool INTERLEAVED = decltype(inter)::value;
+    if (p.q_norm || p.k_norm) hipLaunchKernelGGL((rotate_kernel<D, INTERLEAVED, KIND, true>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, st, p);
+    else hipLaunchKernelGGL((rotate_kernel<D, INTERLEAVED, KIND, false>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, st, p);
   };
   auto shape = [&](auto d) {
     if (a->interleaved) go(d, std::true_type{});
