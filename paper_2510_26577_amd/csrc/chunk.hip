@@ -694,21 +694,41 @@ struct ChunkPlan {
   int blocks;
   int parts, part_keys;
 };
+// Rows of a workgroup.  Up to 32 rows of a sequence: 32.  More: 32 all the same where the keys are few and one round of workgroups holds them
+// (a chunk of 512 tokens alone 14.6 us, with 128 rows 19.1; of 200 behind 200 others 17.7 and 18.1; but 512 behind 4096 94 and 59).  256 rows,
+// which bring half as many tiles as 128, where there are workgroups for every compute unit whose keys are about as many (2048 tokens behind
+// 30000: 948 us, with 128 rows 1058; 8192 in a window of 4096 525 and 560), or for several rounds; a prompt's first chunk has row blocks of
+// one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 59 us, with 256 rows 64).
+// Parts: two launches cost 3 to 4 us more than one, and a partial row is written and read again.  32 rows, four waves to a workgroup, each with
+// tiles of its own: one workgroup per CU, two where they are long (one token behind 4096 in 32 parts 14.0 us, in 64 15.5; 32 sequences of 4096 in
+// 2 parts 105, in 1 140), two tiles at least.  128 rows: two per CU, three tiles at least (60 nodes behind 8192 in a window of 4096: 16
+// parts 22.6 us, 32 27.7).
 void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
+  constexpr int kCUs = 256, kFewKeys = 512, kLongPart = 64;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
-  pl->rows = a->plan_rows ? a->plan_rows : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
-  pl->KT = pl->rows == 32 ? 32 : 64;
-  const int64_t blocks = (int64_t)a->sum_T * G / pl->rows + a->B;
-  pl->blocks = (int)std::min<int64_t>(blocks, 0x7fffffff);
-  // keys that a row block may see
-  const int64_t seen = a->window ? std::min<int64_t>((int64_t)a->max_L + a->max_T, (int64_t)a->window + a->n_first + pl->rows / G + 2 * pl->KT) : (int64_t)a->max_L + a->max_T;
-  const int64_t tiles = std::max<int64_t>(1, (seen + pl->KT - 1) / pl->KT);
-  const int slots = pl->rows == 256 ? 256 : 512;
   // row blocks that have rows: a sequence of max_T tokens has this many
-  const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(blocks, (int64_t)a->B * ((rows + pl->rows - 1) / pl->rows))) * a->Hkv;
+  auto busy_with = [&](int R) {
+    const int64_t of_rows = (int64_t)a->sum_T * G / R + a->B, of_sequences = (int64_t)a->B * ((rows + R - 1) / R);
+    return std::max<int64_t>(1, std::min(of_rows, of_sequences)) * a->Hkv;
+  };
+  const int64_t all = (int64_t)a->max_L + a->max_T;
+  auto seen_with = [&](int R, int KT) { return a->window ? std::min<int64_t>(all, (int64_t)a->window + a->n_first + R / G + 2 * KT) : all; };
+  if (a->plan_rows) pl->rows = a->plan_rows;
+  else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && seen_with(32, 32) <= kFewKeys)) pl->rows = 32;
+  else if (busy_with(256) >= 4 * kCUs || (busy_with(256) >= kCUs && a->max_L >= a->max_T)) pl->rows = 256;
+  else pl->rows = 128;
+  pl->KT = pl->rows == 32 ? 32 : 64;
+  pl->blocks = (int)std::min<int64_t>((int64_t)a->sum_T * G / pl->rows + a->B, 0x7fffffff);
+  const int64_t busy = busy_with(pl->rows), tiles = std::max<int64_t>(1, (seen_with(pl->rows, pl->KT) + pl->KT - 1) / pl->KT);
   int64_t parts = a->num_splits;
-  if (parts == 0) parts = busy >= 2 * slots ? 1 : std::max<int64_t>(1, slots / busy);
+  if (parts == 0 && pl->rows == 32) {
+    parts = std::max<int64_t>(1, kCUs / busy);
+    if (tiles / parts >= kLongPart) parts = std::max<int64_t>(1, 2 * kCUs / busy);
+    parts = std::min(parts, std::max<int64_t>(1, tiles / 2));
+  } else if (parts == 0) {
+    parts = std::min(std::max<int64_t>(1, (pl->rows == 128 ? 2 : 1) * kCUs / busy), std::max<int64_t>(1, tiles / 3));
+  }
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, tiles));
   pl->part_keys = (int)((tiles + parts - 1) / parts) * pl->KT;
   pl->parts = (int)parts;
