@@ -74,8 +74,8 @@ size_t tva_sizeof_rotate_args(void);
  *   BF16  as it is;  E4M3  the nearest code to the fp32 quotient by k_scale / v_scale (ties to even), magnitudes above 448
  *   become 448, infinities among them, NaN becomes 0;  E2M1  as tva_cache_store rounds it.
  * r.k is required, r.k_out may be NULL or get the turned keys besides; r.q may be NULL.  r.cu_T and r.L are required.
- * A position outside the sequence's room is left out and, if err_flag is given (zero on entry), stores 1 + b there.
- * L_out[b] = L[b] + T_b if given (not L itself).
+ * A position outside the sequence's room, or whose entry in the page table is below 0, is left out and, if err_flag is given (zero on
+ * entry), stores 1 + b there.  Pages (rows) that are reached belong to one sequence.  L_out[b] = L[b] + T_b if given (not L itself).
  */
 typedef struct tva_append_args {
   tva_rotate_args r;
@@ -101,7 +101,9 @@ size_t tva_sizeof_append_args(void);
  * out is bf16, rounded once from fp32; lse fp32, natural logarithm, may be NULL.  Sums and softmax weights are fp32; as a factor of V
  * a weight is rounded to bf16 (half a step, 2^-8 of it at most), with plan_rows 32 to 16 bits.  A row that sees nothing gets out = 0,
  * lse = -inf.  A key or value that is not finite reaches the rows that see it, and no others.  Rows from cu_T[B] on are left as they
- * are.  Positions outside the sequence's room are not read.  E2M1 caches are read by tva_tree_verify_attn_4bit: TVA_UNSUPPORTED here.
+ * are.  Positions outside the sequence's room are not read; a page
+ * none of whose positions any token sees may have an entry below 0 in the page table (given back: page 0 is read in its place, to no
+ * effect), others below L[b] + T_b are pages.  E2M1 caches are read by tva_tree_verify_attn_4bit: TVA_UNSUPPORTED here.
  * max_T and max_L size the launch: rows i >= max_T are not computed; max_L only shapes the plan.
  * The workspace holds partial results where keys are split (0 bytes when nothing is); what it holds before does not matter, and
  * calls that overlap need one each.

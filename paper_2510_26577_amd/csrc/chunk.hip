@@ -248,14 +248,15 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   const uint32_t row_bytes = (uint32_t)(p.c.stride_tok * BYTES);
   // (a tile past the last one: the last again.  A branch would leave the waits without a count to go by)
   auto first_slot = [&](int u) __attribute__((always_inline)) { return tiles.at(min(u, u1 - 1)) * C::KT; };
+  // (an entry below 0, a page given back that the window has left: its rows share a tile with rows that are seen; page 0 is read for it)
   auto look = [&](int u) __attribute__((always_inline)) {
     const int t = first_slot(u);
     if constexpr (PLACES == kRows) {
 #pragma unroll
-      for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last));
+      for (int i = 0; i < C::NP; ++i) entry[i] = max(find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last)), 0);
     } else if constexpr (PLACES == kPages) {
       const int row = min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group), page = page_of(p.c, row);
-      entry[0] = find.table[page], in_page = (uint32_t)(row - page * p.c.page_size) * row_bytes;
+      entry[0] = max(find.table[page], 0), in_page = (uint32_t)(row - page * p.c.page_size) * row_bytes;
     }
   };
   auto locate = [&](int u) __attribute__((always_inline)) {

@@ -166,6 +166,8 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
   if constexpr (KIND != kNoCache) {
     const int64_t slot = (int64_t)start + i;
     room = slot >= 0 && slot < room_of(p.c, b);
+    // (a table's entry below 0 is no page: what a table is filled with behind a sequence's pages)
+    if (room && p.c.page_table) room = p.c.page_table[(int64_t)b * p.c.max_pages + page_of(p.c, (int)slot)] >= 0;
     if (room) at_cache = position_at(p.c, b, (int)slot);
     else if (p.err_flag && first <= p.q_pieces && lane == 0) atomicCAS(p.err_flag, 0, 1 + b);
   }
