@@ -38,6 +38,7 @@ struct ChunkParams {
   float *part_out, *part_lse;  // [blocks, parts, Hkv, rows of a block, D], [blocks, parts, Hkv, rows]
   int64_t q_stride;
   int B, Hq, Hkv, G, W, blocks, max_T;
+  int each;  // row blocks that every sequence has, 0: as many as its rows need (Block)
   int parts, part_keys;  // the most parts a block's tiles are cut into, and the keys of a part that it is cut for
   int window, n_first;   // window: 2^30 where there is none
   int longest;           // row blocks that are taken from the last on, before the others from the first on
@@ -48,18 +49,26 @@ struct ChunkParams {
 __device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // A row block of one sequence: where its rows and its keys lie.
-// Blocks are numbered so that a sequence's first is known from cu_T alone: floor(cu_T[b] G / rows) + b.  A sequence of n rows has
-// ceil(n / rows) of the numbers up to the next one's first, which are at least that many.
+// Blocks are numbered so that a sequence's first is known: `each` times b, or from cu_T alone floor(cu_T[b] G / rows) + b: a sequence of n
+// rows has ceil(n / rows) of the numbers up to the next one's first, which are at least that many.  The launch takes what gives fewer: the
+// numbers without rows leave compute units idle where one workgroup for each was asked for (four trees of 60 nodes, 11 numbers for 8 blocks).
 struct Block {
   int b, t0, T, L;
   int row0, rows;  // first row (token x head of the KV head) of the sequence, rows of this block
   int low, high;   // bounds of the positions that the rows have
   int end;         // key slots that a row may see
   __device__ __forceinline__ Block(const ChunkParams &p, int R, int number) {
-    auto first = [&](int n, int row) __attribute__((always_inline)) { return (int64_t)row * p.G / R + n; };
-    const sequences::Place place = sequences::find(p.cu_T, p.L, p.B, number, first);
-    b = same(place.b), t0 = same(place.t0), T = same(min(place.t1 - place.t0, p.max_T)), L = same(max(place.L, 0));
-    const int64_t at = (int64_t)(number - first(b, t0)) * R, all = (int64_t)T * p.G;
+    int64_t from;  // the number of its first one
+    if (p.each) {
+      b = same((int)((uint32_t)number / (uint32_t)p.each)), from = (int64_t)b * p.each;
+      t0 = p.cu_T[b], T = p.cu_T[b + 1] - t0, L = p.L[b];
+    } else {
+      auto first = [&](int n, int row) __attribute__((always_inline)) { return (int64_t)row * p.G / R + n; };
+      const sequences::Place place = sequences::find(p.cu_T, p.L, p.B, number, first);
+      b = same(place.b), t0 = same(place.t0), T = place.t1 - place.t0, L = place.L, from = first(b, t0);
+    }
+    T = same(min(T, p.max_T)), L = same(max(L, 0));
+    const int64_t at = (number - from) * R, all = (int64_t)T * p.G;
     rows = same((int)max((int64_t)0, min((int64_t)R, all - at)));
     row0 = same((int)min(at, all));
     const int64_t room = room_of(p.c, b);
@@ -692,20 +701,22 @@ __global__ void __launch_bounds__(256) merge_kernel(const ChunkParams p, int KT)
 
 struct ChunkPlan {
   int rows, KT;    // of a workgroup, keys of its tiles
-  int blocks;
+  int blocks, each;  // row blocks (ChunkParams)
   int parts, part_keys;
 };
-// Rows of a workgroup.  Up to 32 rows of a sequence: 32.  More: 32 all the same where the keys are few and one round of workgroups holds them
-// (a chunk of 512 tokens alone 14.6 us, with 128 rows 19.1; of 200 behind 200 others 17.7 and 18.1; but 512 behind 4096 94 and 59).  256 rows,
-// which bring half as many tiles as 128, where there are workgroups for every compute unit whose keys are about as many (2048 tokens behind
-// 30000: 948 us, with 128 rows 1058; 8192 in a window of 4096 525 and 560), or for several rounds; a prompt's first chunk has row blocks of
-// one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 59 us, with 256 rows 64).
-// Parts: two launches cost 3 to 4 us more than one, and a partial row is written and read again.  32 rows, four waves to a workgroup, each with
-// tiles of its own: one workgroup per CU, two where they are long (one token behind 4096 in 32 parts 14.0 us, in 64 15.5; 32 sequences of 4096 in
-// 2 parts 105, in 1 140), two tiles at least.  128 rows: two per CU, three tiles at least (60 nodes behind 8192 in a window of 4096: 16
-// parts 22.6 us, 32 27.7).
+// Rows of a workgroup.  Up to 32 rows of a sequence: 32.  More: 32 all the same where two rounds of workgroups hold them and a part has few keys
+// (512 tokens alone 14.5 us, with 128 rows 21.6; 256 behind 512 16.3 and 20.1; 30 behind 5000 18.7 and 20.6; but 128 behind 1500 22.4 and
+// 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where their keys are about as many and there are
+// workgroups for every compute unit (2048 tokens behind 30000: 948 us, with 128 rows 1058; 8192 in a window of 4096 525 and 560) or 128 rows
+// would have long parts and as good as twice the blocks (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind 4096 166 and
+// 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90), or for several rounds; a prompt's first chunk has row blocks
+// of one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 55 us, with 256 rows 60).
+// Parts: two launches cost 3 to 4 us more than one, and a partial row is written and read again.  One workgroup per CU, two where a part is long
+// (32 rows, four waves to a workgroup, each with tiles of its own: one token behind 4096 in 32 parts 14.0 us, in 64 15.5; 32 sequences of 4096 in
+// 2 parts 105, in 1 140.  128 rows: 60 nodes behind 4096 in 16 parts 23.3, in 32 26.5, behind 16384 39.3 and 41.4; 30 tokens behind 32768 in 32
+// parts 41, in 64 46; four times 60 behind 16384 in 4 parts 112, in 8 101), of two tiles at least.
 void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
-  constexpr int kCUs = 256, kFewKeys = 512, kLongPart = 64;
+  constexpr int kCUs = 256, kFewKeys = 768, kLongPart = 64, kLongPart128 = 24;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
   // row blocks that have rows: a sequence of max_T tokens has this many
@@ -715,12 +726,15 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   };
   const int64_t all = (int64_t)a->max_L + a->max_T;
   auto seen_with = [&](int R, int KT) { return a->window ? std::min<int64_t>(all, (int64_t)a->window + a->n_first + R / G + 2 * KT) : all; };
+  const bool long_with_128 = seen_with(128, 64) / 64 / std::max<int64_t>(1, kCUs / busy_with(128)) >= kLongPart128 && busy_with(128) <= 2 * kCUs;
   if (a->plan_rows) pl->rows = a->plan_rows;
-  else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && seen_with(32, 32) <= kFewKeys)) pl->rows = 32;
-  else if (busy_with(256) >= 4 * kCUs || (busy_with(256) >= kCUs && a->max_L >= a->max_T)) pl->rows = 256;
+  else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && seen_with(32, 32) <= kFewKeys * std::max<int64_t>(1, kCUs / busy_with(32)))) pl->rows = 32;
+  else if (busy_with(256) >= 4 * kCUs || (a->max_L >= a->max_T && (busy_with(256) >= kCUs || (2 * busy_with(256) <= busy_with(128) && long_with_128)))) pl->rows = 256;
   else pl->rows = 128;
   pl->KT = pl->rows == 32 ? 32 : 64;
-  pl->blocks = (int)std::min<int64_t>((int64_t)a->sum_T * G / pl->rows + a->B, 0x7fffffff);
+  const int64_t by_rows = (int64_t)a->sum_T * G / pl->rows + a->B, each = (rows + pl->rows - 1) / pl->rows, by_sequences = a->B * each;
+  pl->each = by_sequences <= by_rows ? (int)each : 0;
+  pl->blocks = (int)std::min<int64_t>(std::min(by_rows, by_sequences), 0x7fffffff);
   const int64_t busy = busy_with(pl->rows), tiles = std::max<int64_t>(1, (seen_with(pl->rows, pl->KT) + pl->KT - 1) / pl->KT);
   int64_t parts = a->num_splits;
   if (parts == 0 && pl->rows == 32) {
@@ -728,7 +742,9 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
     if (tiles / parts >= kLongPart) parts = std::max<int64_t>(1, 2 * kCUs / busy);
     parts = std::min(parts, std::max<int64_t>(1, tiles / 2));
   } else if (parts == 0) {
-    parts = std::min(std::max<int64_t>(1, (pl->rows == 128 ? 2 : 1) * kCUs / busy), std::max<int64_t>(1, tiles / 3));
+    parts = std::max<int64_t>(1, kCUs / busy);
+    if (pl->rows == 128 && tiles / parts >= kLongPart128) parts = std::max<int64_t>(1, 2 * kCUs / busy);
+    parts = std::min(parts, std::max<int64_t>(1, tiles / 2));
   }
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, tiles));
   pl->part_keys = (int)((tiles + parts - 1) / parts) * pl->KT;
@@ -802,7 +818,7 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
   p.out = (__bf16 *)a->out, p.lse = a->lse;
   p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (need ? need / 4 / (a->D + 1) * a->D : 0);
   p.q_stride = a->q_stride ? a->q_stride : (int64_t)a->Hq * a->D;
-  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.blocks = pl.blocks, p.max_T = a->max_T;
+  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.blocks = pl.blocks, p.each = pl.each, p.max_T = a->max_T;
   p.parts = pl.parts, p.part_keys = pl.part_keys;
   p.window = a->window ? std::min(a->window, 1 << 30) : 1 << 30, p.n_first = a->window ? a->n_first : 0;
   p.scale_log2 = a->scale * kLog2e * k_scale, p.v_scale = !eight || a->cache.v_scale == 0.f ? 1.f : a->cache.v_scale;

@@ -94,9 +94,9 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (KIND != kNoCache && blockIdx.x == 0 && p.L_out)
     for (int b = threadIdx.x; b < p.B; b += 64 * kWaves) p.L_out[b] = p.L[b] + (p.cu_T[b + 1] - p.cu_T[b]);
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
-  const int64_t row = unit / p.parts;
-  const int first = (int)(unit - row * p.parts) * U;
+  const uint32_t unit = blockIdx.x * kWaves + wave;
+  const int64_t row = unit / (uint32_t)p.parts;
+  const int first = (int)(unit - (uint32_t)row * (uint32_t)p.parts) * U;
   if (row >= p.sum_T) return;
   const int piece = lane % LPR;  // of the head: elements 8 piece ..
   const int half = p.dims / 16;  // pieces between the two elements of a pair
@@ -260,7 +260,7 @@ template <int KIND>
 int launch(const tva_rotate_args *a, RotateParams &p, hipStream_t st) {
   p.parts = std::max(1, (p.q_pieces + p.k_pieces + p.v_pieces + kRowsInFlight - 1) / kRowsInFlight);
   const int64_t blocks = std::max<int64_t>(1, ((int64_t)p.sum_T * p.parts + kWaves - 1) / kWaves);
-  if (blocks > 0x7fffffff) return TVA_UNSUPPORTED;
+  if (blocks > 0x3fffffff) return TVA_UNSUPPORTED;  // (waves are numbered in 32 bits)
   (void)hipGetLastError();
   auto go = [&](auto d, auto inter) {
     constexpr int D = decltype(d)::value;
