@@ -38,7 +38,8 @@ struct ChunkParams {
   float *part_out, *part_lse;  // [blocks, parts, Hkv, rows of a block, D], [blocks, parts, Hkv, rows]
   int64_t q_stride;
   int B, Hq, Hkv, G, W, blocks, max_T;
-  int each;  // row blocks that every sequence has, 0: as many as its rows need (Block)
+  bool by_keys;  // how row blocks are numbered (Block)
+  int each;
   int parts, part_keys;  // the most parts a block's tiles are cut into, and the keys of a part that it is cut for
   int window, n_first;   // window: 2^30 where there is none
   int longest;           // row blocks that are taken from the last on, before the others from the first on
@@ -49,9 +50,14 @@ struct ChunkParams {
 __device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // A row block of one sequence: where its rows and its keys lie.
-// Blocks are numbered so that a sequence's first is known: `each` times b, or from cu_T alone floor(cu_T[b] G / rows) + b: a sequence of n
-// rows has ceil(n / rows) of the numbers up to the next one's first, which are at least that many.  The launch takes what gives fewer: the
-// numbers without rows leave compute units idle where one workgroup for each was asked for (four trees of 60 nodes, 11 numbers for 8 blocks).
+// Blocks are numbered in one of three ways, of which the launch takes one:
+//   by their keys  up to 64 sequences: those with the most keys first, and of each its last block, which sees the most, first.  A lane per
+//                  sequence finds where its blocks begin.  (16 sequences of 1 to 333 tokens behind 100 to 8000, 8-bit rows: 201 us, by rows 259)
+//   evenly         `each` for every sequence
+//   by rows        a sequence's first is floor(cu_T[b] G / rows) + b: one of n rows has ceil(n / rows) of the numbers up to the next one's first,
+//                  which are at least that many
+// (Numbers without rows leave compute units idle where one workgroup for each was asked for: four trees of 60 nodes, 11 numbers by rows for 8
+// blocks, 51 and 39 us.)
 struct Block {
   int b, t0, T, L;
   int row0, rows;  // first row (token x head of the KV head) of the sequence, rows of this block
@@ -59,7 +65,21 @@ struct Block {
   int end;         // key slots that a row may see
   __device__ __forceinline__ Block(const ChunkParams &p, int R, int number) {
     int64_t from;  // the number of its first one
-    if (p.each) {
+    if (p.by_keys) {
+      const int lane = threadIdx.x & 63, n = min(lane, p.B - 1), begin = p.cu_T[n], tokens = max(0, min(p.cu_T[n + 1] - begin, p.max_T)), cached = max(p.L[n], 0);
+      const int blocks = lane < p.B ? (int)(((int64_t)tokens * p.G + R - 1) / R) : 0, keys = min(cached, p.window) + tokens;
+      int start = 0;
+#pragma unroll 4
+      for (int x = 0; x < p.B; ++x) {
+        const int other = __builtin_amdgcn_readlane(keys, x), many = __builtin_amdgcn_readlane(blocks, x);
+        start += other > keys || (other == keys && x < lane) ? many : 0;
+      }
+      const uint64_t here = __ballot(number >= start && number < start + blocks);
+      b = here ? __builtin_ctzll(here) : 0;
+      t0 = __builtin_amdgcn_readlane(begin, b), T = __builtin_amdgcn_readlane(tokens, b), L = __builtin_amdgcn_readlane(cached, b);
+      from = number - (__builtin_amdgcn_readlane(blocks, b) - 1 - (number - __builtin_amdgcn_readlane(start, b)));
+      if (!here) T = 0, from = number;  // behind the last block: no rows
+    } else if (p.each) {
       b = same((int)((uint32_t)number / (uint32_t)p.each)), from = (int64_t)b * p.each;
       t0 = p.cu_T[b], T = p.cu_T[b + 1] - t0, L = p.L[b];
     } else {
@@ -701,16 +721,19 @@ __global__ void __launch_bounds__(256) merge_kernel(const ChunkParams p, int KT)
 
 struct ChunkPlan {
   int rows, KT;    // of a workgroup, keys of its tiles
-  int blocks, each;  // row blocks (ChunkParams)
+  bool by_keys;  // row blocks (Block)
+  int blocks, each;
   int parts, part_keys;
 };
 // Rows of a workgroup.  Up to 32 rows of a sequence: 32.  More: 32 all the same where two rounds of workgroups hold them and a part has few keys
 // (512 tokens alone 14.5 us, with 128 rows 21.6; 256 behind 512 16.3 and 20.1; 30 behind 5000 18.7 and 20.6; but 128 behind 1500 22.4 and
-// 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where their keys are about as many and there are
-// workgroups for every compute unit (2048 tokens behind 30000: 948 us, with 128 rows 1058; 8192 in a window of 4096 525 and 560) or 128 rows
-// would have long parts and as good as twice the blocks (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind 4096 166 and
-// 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90), or for several rounds; a prompt's first chunk has row blocks
-// of one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 55 us, with 256 rows 60).
+// 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where 128 rows have twice the
+// blocks, their keys are about as many and there are workgroups for every compute unit (2048 tokens behind 30000: 948 us, with 128 rows 1058;
+// 8192 in a window of 4096 525 and 560) or 128 rows would have long parts (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind 4096 166 and
+// 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90, 16 ragged ones of 1 to 333 behind 100 to 8000 223 and 201, 70 of 1 to 30 behind up to 300 46 and 30), or where
+// there are several rounds of blocks with many keys (4096 tokens 150 and 165; 10 times 2048 440 and 465; but 20 times 512 108 and 97, 70 ragged ones
+// of 1 to 120 behind up to 3000 252 and 215).  A prompt's first chunk has row blocks of one tile to all, which two 128-row workgroups per CU
+// level out (2048 tokens: 54 us, with 256 rows 63).  (A batch whose longest sequence is alone with its length waits for it: max_L says no more.)
 // Parts: two launches cost 3 to 4 us more than one, and a partial row is written and read again.  One workgroup per CU, two where a part is long
 // (32 rows, four waves to a workgroup, each with tiles of its own: one token behind 4096 in 32 parts 14.0 us, in 64 15.5; 32 sequences of 4096 in
 // 2 parts 105, in 1 140.  128 rows: 60 nodes behind 4096 in 16 parts 23.3, in 32 26.5, behind 16384 39.3 and 41.4; 30 tokens behind 32768 in 32
@@ -719,22 +742,22 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   constexpr int kCUs = 256, kFewKeys = 768, kLongPart = 64, kLongPart128 = 24;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
-  // row blocks that have rows: a sequence of max_T tokens has this many
-  auto busy_with = [&](int R) {
-    const int64_t of_rows = (int64_t)a->sum_T * G / R + a->B, of_sequences = (int64_t)a->B * ((rows + R - 1) / R);
-    return std::max<int64_t>(1, std::min(of_rows, of_sequences)) * a->Hkv;
-  };
+  // row blocks of R rows: as many as the rows need (and one more for a sequence), or evenly as many as max_T tokens do
+  auto by_rows = [&](int R) { return (int64_t)a->sum_T * G / R + a->B; };
+  auto by_sequences = [&](int R) { return (int64_t)a->B * ((rows + R - 1) / R); };
+  auto even = [&](int R) { return by_sequences(R) <= by_rows(R); };
+  auto busy_with = [&](int R) { return std::max<int64_t>(1, std::min(by_rows(R), by_sequences(R))) * a->Hkv; };
   const int64_t all = (int64_t)a->max_L + a->max_T;
   auto seen_with = [&](int R, int KT) { return a->window ? std::min<int64_t>(all, (int64_t)a->window + a->n_first + R / G + 2 * KT) : all; };
   const bool long_with_128 = seen_with(128, 64) / 64 / std::max<int64_t>(1, kCUs / busy_with(128)) >= kLongPart128 && busy_with(128) <= 2 * kCUs;
   if (a->plan_rows) pl->rows = a->plan_rows;
   else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && seen_with(32, 32) <= kFewKeys * std::max<int64_t>(1, kCUs / busy_with(32)))) pl->rows = 32;
-  else if (busy_with(256) >= 4 * kCUs || (a->max_L >= a->max_T && (busy_with(256) >= kCUs || (2 * busy_with(256) <= busy_with(128) && long_with_128)))) pl->rows = 256;
+  else if (rows >= 1024 && a->max_L + a->max_T / 2 >= 512 && busy_with(256) >= (even(256) ? 3 * kCUs / 2 : 4 * kCUs)) pl->rows = 256;
+  else if (a->max_L >= a->max_T && 2 * busy_with(256) <= busy_with(128) && ((busy_with(256) >= kCUs && even(256)) || long_with_128)) pl->rows = 256;
   else pl->rows = 128;
   pl->KT = pl->rows == 32 ? 32 : 64;
-  const int64_t by_rows = (int64_t)a->sum_T * G / pl->rows + a->B, each = (rows + pl->rows - 1) / pl->rows, by_sequences = a->B * each;
-  pl->each = by_sequences <= by_rows ? (int)each : 0;
-  pl->blocks = (int)std::min<int64_t>(std::min(by_rows, by_sequences), 0x7fffffff);
+  pl->each = even(pl->rows) ? (int)((rows + pl->rows - 1) / pl->rows) : 0;
+  pl->blocks = (int)std::min<int64_t>(std::min(by_rows(pl->rows), by_sequences(pl->rows)), 0x7fffffff);
   const int64_t busy = busy_with(pl->rows), tiles = std::max<int64_t>(1, (seen_with(pl->rows, pl->KT) + pl->KT - 1) / pl->KT);
   int64_t parts = a->num_splits;
   if (parts == 0 && pl->rows == 32) {
@@ -749,6 +772,9 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, tiles));
   pl->part_keys = (int)((tiles + parts - 1) / parts) * pl->KT;
   pl->parts = (int)parts;
+  // (even batches gain nothing by the order and pay for it: 64 single tokens in a window of 1024 57 us, by their keys 62; lengths of 100 to 16000
+  // 426 and 427)
+  pl->by_keys = a->B > 1 && a->B <= 64 && !pl->each;
 }
 
 int check_chunk(const tva_chunk_args *a, bool shapes_only) {
@@ -818,12 +844,12 @@ int tva_chunk_attn(const tva_chunk_args *a, void *stream) {
   p.out = (__bf16 *)a->out, p.lse = a->lse;
   p.part_out = (float *)a->workspace, p.part_lse = p.part_out + (need ? need / 4 / (a->D + 1) * a->D : 0);
   p.q_stride = a->q_stride ? a->q_stride : (int64_t)a->Hq * a->D;
-  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.blocks = pl.blocks, p.each = pl.each, p.max_T = a->max_T;
+  p.B = a->B, p.Hq = a->Hq, p.Hkv = a->Hkv, p.G = a->Hq / a->Hkv, p.W = a->mask_words, p.blocks = pl.blocks, p.by_keys = pl.by_keys, p.each = pl.each, p.max_T = a->max_T;
   p.parts = pl.parts, p.part_keys = pl.part_keys;
   p.window = a->window ? std::min(a->window, 1 << 30) : 1 << 30, p.n_first = a->window ? a->n_first : 0;
   p.scale_log2 = a->scale * kLog2e * k_scale, p.v_scale = !eight || a->cache.v_scale == 0.f ? 1.f : a->cache.v_scale;
   const int first_round = 256 / a->Hkv;
-  p.longest = pl.rows == 128 && pl.parts == 1 && pl.blocks > first_round && pl.blocks <= 2 * first_round ? first_round : pl.blocks;
+  p.longest = pl.by_keys ? 0 : pl.rows == 128 && pl.parts == 1 && pl.blocks > first_round && pl.blocks <= 2 * first_round ? first_round : pl.blocks;
   const dim3 grid(a->Hkv, pl.parts, pl.blocks);
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();

@@ -240,3 +240,22 @@ def test_rows_beyond_the_bound_are_not_computed(torch):
 def test_one_long_chunk(torch):
     _attend(torch, np.random.default_rng(16), (8, 2, 128), [1100], [900], 64)
     _attend(torch, np.random.default_rng(17), (4, 1, 64), [1500], [37], 16, window=333, n_first=4, rows="e4m3")
+
+
+@pytest.mark.parametrize("plan", [32, 128, 256])
+@pytest.mark.parametrize("B,kind", [(2, "alone"), (5, "alone"), (64, "alone"), (65, "alone"), (12, "even"), (9, "ragged"), (64, "ragged"), (66, "ragged"), (7, "bounded")])
+def test_blocks_of_batches(torch, B, kind, plan):
+    """Row blocks are numbered by keys, evenly or by rows: each is computed once, whatever the sequences' lengths."""
+    rng = np.random.default_rng(1000 * B + plan)
+    sizes, lengths, more = rng.integers(1, 40, B), rng.integers(0, 200, B), {}
+    if kind == "alone":  # all but one have no tokens
+        sizes[:] = 0
+        sizes[rng.integers(B)] = 150
+    elif kind == "even":
+        sizes[:], lengths[::2] = 70, 33
+    elif kind == "ragged":
+        sizes[rng.integers(0, B, 3)] = 0, 131, 97
+        lengths[:3] = 180  # (keys alike)
+    else:
+        more = dict(max_T=500, padded=800)
+    _attend(torch, rng, (4, 1, 64), sizes.tolist(), lengths.tolist(), 16, plan=plan, splits=1 + B % 3, **more)
