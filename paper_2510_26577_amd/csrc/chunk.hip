@@ -1,12 +1,20 @@
 // libtva: attention of new tokens over the cache that holds them (gfx950).  Entry points and their meaning: include/tva_layer.h.
 //
-//   chunk_kernel  S^T = K Q^T and O^T = V^T P^T by 32x32x16 bf16 MFMAs, a query row per lane of a half, as in tva.hip and cache4.hip.
-//                 A workgroup has 32 * WM query rows (tokens x heads of a KV head: the heads share the keys) and walks tiles of
-//                 32 * KB * WK keys; its waves are WM row groups x WK key groups.  All waves bring a tile to LDS (through registers,
-//                 two tiles ahead; 8-bit rows are widened on the way) and read their operands there: K as rows, V by transposing
-//                 reads.  Only tiles that some row sees are walked: the first ones (of n_first), then those of the window or all.
+//   chunk_kernel  S^T = K Q^T and O^T = V^T P^T by 32x32x16 bf16 MFMAs, a query row per lane of a half, as in tva.hip and cache4.hip:
+//                 the scores of a row then lie in the registers that the second product takes its weights from, and a row's maximum and
+//                 sum are one lane exchange.  One pass over the keys with the running maximum and sum of the softmax.  A workgroup has
+//                 32, 128 or 256 query rows (tokens x heads of a KV head: the heads share the keys) and walks tiles of its keys; only
+//                 tiles that some row sees are walked: the first ones (of n_first), then those of the window or all.
 //   merge_kernel  partial results of row blocks whose keys were split.
-// A block's tiles are cut into equal parts, as many as the plan's length of a part asks for.
+//
+// 32 rows (single tokens, few new ones) wait for memory: four waves, each with 32-key tiles of its own that it brings and waits for alone, its
+// next one on the way meanwhile.  64 sequences of 1024 seen keys: 56 us, 4.8 TB/s; 256 of 4096: 722 us, 5.9 TB/s (a copy: 5.1).
+// 128 and 256 rows are bound by the instructions of a tile: all waves bring 64-key tiles to LDS together (through registers, K two tiles ahead;
+// 8-bit rows are widened on the way) and read their operands there, K as rows, V by transposing reads.  2048 tokens behind 30000: 965 us,
+// 1.08 PFLOP/s (a library product of 8192^3: 1.26 to 1.36); per matrix instruction, which takes the matrix unit 32 cycles, 5.6 vector
+// instructions and an exponential among them take the vector unit 34, of which it can do 16 under the matrix instruction; the matrix units are
+// busy for 51 % of the cycles, and the chip lowers its clock to 1.7 to 2.0 GHz under that load.  128 rows leave two workgroups to a compute
+// unit, which fill each other's barriers and share long and short blocks; 256 bring every tile half as often.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -69,7 +77,6 @@ struct Block {
       const int lane = threadIdx.x & 63, n = min(lane, p.B - 1), begin = p.cu_T[n], tokens = max(0, min(p.cu_T[n + 1] - begin, p.max_T)), cached = max(p.L[n], 0);
       const int blocks = lane < p.B ? (int)(((int64_t)tokens * p.G + R - 1) / R) : 0, keys = min(cached, p.window) + tokens;
       int start = 0;
-#pragma unroll 4
       for (int x = 0; x < p.B; ++x) {
         const int other = __builtin_amdgcn_readlane(keys, x), many = __builtin_amdgcn_readlane(blocks, x);
         start += other > keys || (other == keys && x < lane) ? many : 0;
@@ -175,8 +182,8 @@ __device__ __forceinline__ void times(F f) {
 }
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block: the last ones, which see the
-// most keys, first; where two workgroups per CU hold them all, the second ones from the first on, so that a long and a short one share a CU.
+// Grid: KV head (fastest: with 8 heads one per XCD, whose L2 then holds one head's keys), part, row block: those that see the most keys first;
+// where two workgroups per CU hold all of one sequence, the second ones from the first on, so that a long and a short one share a CU.
 // PLACES: how a tile's rows are found.  kDense and kPages: the rows that a wave brings at once lie in a sequence, or a page, one after the
 // other: scalar addresses and a lane's offset; kRows: each lane looks for its own (pages that such rows may straddle).
 enum { kDense, kPages, kRows };
@@ -675,7 +682,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
 }
 
 // lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s, D/4 lanes per row, eight parts in flight.
-// Grid: KV head, rows of a block (1024 / D at a time), block.
+// Grid: KV head, rows of a block (1024 / D at a time), block.  (240 rows x 8 heads of 16 parts: 17 MB read, 5.7 us.)
 template <int D, int R>
 __global__ void __launch_bounds__(256) merge_kernel(const ChunkParams p, int KT) {
   constexpr int LPR = D / 4, U = 8, ROWS = 256 / LPR;

@@ -1,10 +1,14 @@
 // libtva: rotary positions, norms of heads, and the append to the cache (gfx950).  Entry points and their meaning:
 // include/tva_layer.h.
 //
-// One kernel, bound by memory: every head is read and written once (what is turned with it is read again, from the cache of
-// the compute unit: half a head away, or in the lane's own 16 bytes).  A wave has one token and up to 16 or 32 heads of it, their
-// rows on the way while the token's position is found and one lane per pair computes its sine and cosine, which all heads share
-// through LDS.
+// One kernel.  Large calls are bound by memory: every head is read once (its pair's half comes from another lane, not from memory) and written
+// once.  A wave has one token and four pieces of 1 KB of its heads (8 lanes of 16 bytes to a head of 64, 16 to one of 128), all on the way while
+// the token's position is found and one lane per pair computes its sine and cosine, which all heads share through LDS.  The grid is token x
+// wave-wide piece in one dimension: with tokens and pieces apart waves start in another order (62 us in the place of 56).
+//   8204 tokens of 64 + 8 heads of 128, half of each turned, interleaved, 288 MB   55 us  5.2 TB/s (a copy: 5.1)
+//   16384 tokens of 32 + 8 heads of 128, normed, 336 MB                            68 us  4.9 TB/s
+//   16396 of 32 + 8 + 8, normed, K and V to 4-bit rows, 352 MB                     87 us  4.0 TB/s (1.26 times the vector instructions)
+// Small calls (a tree's nodes, 64 tokens) are one launch of 4.6 to 5.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
