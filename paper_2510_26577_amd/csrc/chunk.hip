@@ -733,20 +733,22 @@ struct ChunkPlan {
   int parts, part_keys;
 };
 // Rows of a workgroup.  Up to 32 rows of a sequence: 32.  More: 32 all the same where two rounds of workgroups hold them and a part has few keys
-// (512 tokens alone 14.5 us, with 128 rows 21.6; 256 behind 512 16.3 and 20.1; 30 behind 5000 18.7 and 20.6; but 128 behind 1500 22.4 and
-// 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where 128 rows have twice the
+// (512 tokens alone 14.5 us, with 128 rows 21.6, behind 400 23.3 and 28.9; 256 behind 512 16.3 and 20.1; 30 behind 5000 18.7 and 20.6; but 128
+// behind 1500 22.4 and 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where 128 rows have twice the
 // blocks, their keys are about as many and there are workgroups for every compute unit (2048 tokens behind 30000: 948 us, with 128 rows 1058;
-// 8192 in a window of 4096 525 and 560) or 128 rows would have long parts (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind 4096 166 and
-// 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90, 16 ragged ones of 1 to 333 behind 100 to 8000 223 and 201, 70 of 1 to 30 behind up to 300 46 and 30), or where
-// there are several rounds of blocks with many keys (4096 tokens 150 and 165; 10 times 2048 440 and 465; but 20 times 512 108 and 97, 70 ragged ones
-// of 1 to 120 behind up to 3000 252 and 215).  A prompt's first chunk has row blocks of one tile to all, which two 128-row workgroups per CU
-// level out (2048 tokens: 54 us, with 256 rows 63).  (A batch whose longest sequence is alone with its length waits for it: max_L says no more.)
+// 8192 in a window of 4096 525 and 560) or 128 rows would have long parts (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind
+// 4096 166 and 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90, 16 ragged ones of 1 to 333 behind 100 to 8000 223 and
+// 201, 70 of 1 to 30 behind up to 300 46 and 30), or where there are several rounds of blocks with many keys (4096 tokens 150 and 165; 10 times
+// 2048 440 and 465; but 20 times 512 108 and 97, 70 ragged ones of 1 to 120 behind up to 3000 252 and 215).  A prompt's first chunk has row
+// blocks of one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 54 us, with 256 rows 63).  (A batch whose longest
+// sequence is alone with its length waits for it: max_L says no more.)
 // Parts: two launches cost 3 to 4 us more than one, and a partial row is written and read again.  One workgroup per CU, two where a part is long
 // (32 rows, four waves to a workgroup, each with tiles of its own: one token behind 4096 in 32 parts 14.0 us, in 64 15.5; 32 sequences of 4096 in
 // 2 parts 105, in 1 140.  128 rows: 60 nodes behind 4096 in 16 parts 23.3, in 32 26.5, behind 16384 39.3 and 41.4; 30 tokens behind 32768 in 32
-// parts 41, in 64 46; four times 60 behind 16384 in 4 parts 112, in 8 101), of two tiles at least.
+// parts 41, in 64 46; four times 60 behind 16384 in 4 parts 112, in 8 101), of two tiles at least.  A join has to save its 32-row block some
+// tiles: 16 tokens behind 600 in 2 parts 15.9 us, in one 14.1, twice 120 alone 11.5 and 7.7; one behind 512 in 8 parts 9.4, in one 12.9.
 void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
-  constexpr int kCUs = 256, kFewKeys = 768, kLongPart = 64, kLongPart128 = 24;
+  constexpr int kCUs = 256, kFewKeys = 768, kLongPart = 64, kLongPart128 = 24, kManyKeys = 768, kWorthAJoin = 14;
   const int G = a->Hq / a->Hkv;
   const int64_t rows = (int64_t)a->max_T * G;
   // row blocks of R rows: as many as the rows need (and one more for a sequence), or evenly as many as max_T tokens do
@@ -755,11 +757,13 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
   auto even = [&](int R) { return by_sequences(R) <= by_rows(R); };
   auto busy_with = [&](int R) { return std::max<int64_t>(1, std::min(by_rows(R), by_sequences(R))) * a->Hkv; };
   const int64_t all = (int64_t)a->max_L + a->max_T;
+  // keys that a row sees, at the mean over a chunk
+  const int64_t mean = a->window ? std::min<int64_t>(a->max_L + a->max_T / 2, (int64_t)a->window + a->n_first) : (int64_t)a->max_L + a->max_T / 2;
   auto seen_with = [&](int R, int KT) { return a->window ? std::min<int64_t>(all, (int64_t)a->window + a->n_first + R / G + 2 * KT) : all; };
   const bool long_with_128 = seen_with(128, 64) / 64 / std::max<int64_t>(1, kCUs / busy_with(128)) >= kLongPart128 && busy_with(128) <= 2 * kCUs;
   if (a->plan_rows) pl->rows = a->plan_rows;
-  else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && seen_with(32, 32) <= kFewKeys * std::max<int64_t>(1, kCUs / busy_with(32)))) pl->rows = 32;
-  else if (rows >= 1024 && a->max_L + a->max_T / 2 >= 512 && busy_with(256) >= (even(256) ? 3 * kCUs / 2 : 4 * kCUs)) pl->rows = 256;
+  else if (rows <= 32 || (busy_with(32) <= 2 * kCUs && mean <= kFewKeys * std::max<int64_t>(1, kCUs / busy_with(32)))) pl->rows = 32;
+  else if (rows >= 1024 && mean >= kManyKeys && busy_with(256) >= (even(256) ? 3 * kCUs / 2 : 4 * kCUs)) pl->rows = 256;
   else if (a->max_L >= a->max_T && 2 * busy_with(256) <= busy_with(128) && ((busy_with(256) >= kCUs && even(256)) || long_with_128)) pl->rows = 256;
   else pl->rows = 128;
   pl->KT = pl->rows == 32 ? 32 : 64;
@@ -771,6 +775,7 @@ void plan_chunk(const tva_chunk_args *a, ChunkPlan *pl) {
     parts = std::max<int64_t>(1, kCUs / busy);
     if (tiles / parts >= kLongPart) parts = std::max<int64_t>(1, 2 * kCUs / busy);
     parts = std::min(parts, std::max<int64_t>(1, tiles / 2));
+    if (tiles - tiles / parts < kWorthAJoin) parts = 1;
   } else if (parts == 0) {
     parts = std::max<int64_t>(1, kCUs / busy);
     if (pl->rows == 128 && tiles / parts >= kLongPart128) parts = std::max<int64_t>(1, 2 * kCUs / busy);
