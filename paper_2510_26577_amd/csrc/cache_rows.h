@@ -30,7 +30,9 @@ struct CacheView {
 };
 
 // t / page_size, exact for t below 2^30 (page_magic is 2^(31 + page_bits) / page_size rounded up, 2^page_bits >= page_size)
-__device__ __forceinline__ int page_of(const CacheView &c, int t) { return (int)(__umulhi((uint32_t)t * 2u, c.page_magic) >> c.page_bits); }
+__host__ __device__ __forceinline__ int page_of(const CacheView &c, int t) {
+  return (int)((uint32_t)((uint64_t)((uint32_t)t * 2u) * c.page_magic >> 32) >> c.page_bits);
+}
 
 // Where position t of sequence b begins, head 0, in units.  The position is within the sequence's room.
 __device__ __forceinline__ int64_t position_at(const CacheView &c, int b, int t) {
@@ -43,20 +45,25 @@ __device__ __forceinline__ int64_t position_at(const CacheView &c, int b, int t)
 }
 
 // The same for one sequence and head, the look into the page table apart from what is made of it, so that a loop can look ahead:
-// entry() is what is read (nothing in the dense form), at() the place.
-template <bool PAGED>
+// entry() is what is read (nothing in the dense form), at() the place.  GAPS: entries below 0 are allowed among those that are looked up (pages
+// given back): they are page 0 here, so that no place lies outside the cache.
+template <bool PAGED, bool GAPS = false>
 struct Finder {
   const int32_t *table;
   int64_t base;
-  __device__ __forceinline__ Finder(const CacheView &c, int b, int g) {
+  __host__ __device__ __forceinline__ Finder(const CacheView &c, int b, int g) {
     if constexpr (PAGED) table = c.page_table + (int64_t)b * c.max_pages, base = g * c.stride_head;
     else table = nullptr, base = (int64_t)c.cu_L[b] * c.stride_tok + g * c.stride_head;
   }
-  __device__ __forceinline__ int entry(const CacheView &c, int t) const {
-    if constexpr (PAGED) return table[page_of(c, t)];
+  __host__ __device__ __forceinline__ int entry_of(int page) const {
+    if constexpr (!PAGED) return 0;
+    else return GAPS && table[page] < 0 ? 0 : table[page];
+  }
+  __host__ __device__ __forceinline__ int entry(const CacheView &c, int t) const {
+    if constexpr (PAGED) return entry_of(page_of(c, t));
     else return 0;
   }
-  __device__ __forceinline__ int64_t at(const CacheView &c, int t, int entry) const {
+  __host__ __device__ __forceinline__ int64_t at(const CacheView &c, int t, int entry) const {
     if constexpr (PAGED) return base + (int64_t)entry * c.stride_page + (int64_t)(t - page_of(c, t) * c.page_size) * c.stride_tok;
     else return base + (int64_t)t * c.stride_tok;
   }

@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   run_of(low, high, &plain0, &plain1);
 
   // ---- tiles: global memory -> registers -> LDS ----
-  const Finder<PLACES != kDense> find(p.c, k.b, g);
+  const Finder<PLACES != kDense, true> find(p.c, k.b, g);
   const int piece = lane % C::LPR, lrow = lane / C::LPR, bring = C::OWN ? 0 : wave;
   const int last = k.end - 1, last_group = last - last % C::RPW;  // the last slot, and the first of the group that it is in
   constexpr int BYTES = KIND == TVA_ROWS_BF16 ? 2 : 1;            // of an element
@@ -284,15 +284,15 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   const uint32_t row_bytes = (uint32_t)(p.c.stride_tok * BYTES);
   // (a tile past the last one: the last again.  A branch would leave the waits without a count to go by)
   auto first_slot = [&](int u) __attribute__((always_inline)) { return tiles.at(min(u, u1 - 1)) * C::KT; };
-  // (an entry below 0, a page given back that the window has left: its rows share a tile with rows that are seen; page 0 is read for it)
+  // (an entry below 0, a page given back that the window has left: its rows share a tile with rows that are seen; page 0 is read for it: GAPS)
   auto look = [&](int u) __attribute__((always_inline)) {
     const int t = first_slot(u);
     if constexpr (PLACES == kRows) {
 #pragma unroll
-      for (int i = 0; i < C::NP; ++i) entry[i] = max(find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last)), 0);
+      for (int i = 0; i < C::NP; ++i) entry[i] = find.entry(p.c, min(t + (i * C::TOGETHER + bring) * C::RPW + lrow, last));
     } else if constexpr (PLACES == kPages) {
       const int row = min(t + (min(lane, C::NP - 1) * C::TOGETHER + bring) * C::RPW, last_group), page = page_of(p.c, row);
-      entry[0] = max(find.table[page], 0), in_page = (uint32_t)(row - page * p.c.page_size) * row_bytes;
+      entry[0] = find.entry_of(page), in_page = (uint32_t)(row - page * p.c.page_size) * row_bytes;
     }
   };
   auto locate = [&](int u) __attribute__((always_inline)) {
