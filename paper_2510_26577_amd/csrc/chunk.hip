@@ -651,7 +651,8 @@ __global__ void __launch_bounds__(64 * WM *WK, 2) chunk_kernel(const ChunkParams
   if constexpr (WK > 1) __syncthreads();
   else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   // a wave's rows are those of its row group; with several key groups each takes its share of them
-  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, ROUNDS = 32 / WK / AT_ONCE, U = 4;
+  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, ROUNDS = 32 / WK / AT_ONCE, U = ROUNDS < 4 ? ROUNDS : 4;
+  static_assert(ROUNDS % U == 0 && WK * ROUNDS * AT_ONCE == 32, "each row is joined and written by one wave");
   const int d = lane % LANES * 4;
 #pragma unroll 1
   for (int n = 0; n < ROUNDS; n += U) {
