@@ -43,7 +43,8 @@ int tva_rotary_frequencies(int32_t scaling, int32_t dims, double base, double fa
  *            u' = magnitude * (u cos a - v sin a), v' = magnitude * (v cos a + u sin a), a = P * freq[j]; elements from
  *            dims on stay
  * Angles are reduced in 64 bits (any int32 position), sums and products are fp32, the result is rounded to bf16 once.  (A
- * norm's sum of squares is an fp32 number: from 2^128 on it is infinite, and the head becomes 0.)
+ * norm's sum of squares is an fp32 number: from 2^128 on it is infinite, and the head becomes 0, but for elements that are infinite
+ * themselves; with eps 0 a head whose squares all vanish in it has no finite norm.)
  * Rows from cu_T[B] on are left as they are.  q_out may be q with the same stride, k_out k (in place); other
  * overlaps are not allowed.  q or k may be NULL (then so is its output).
  */

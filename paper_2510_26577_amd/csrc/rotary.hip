@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
     head[u] = (is_q ? at : is_k ? at - p.q_pieces : at - p.q_pieces - p.k_pieces) * HEADS + lane / LPR;
     const char *from = is_q ? p.q + row * p.q_stride * 2 : is_k ? p.k + row * p.k_stride * 2 : p.v + row * p.v_stride * 2;
     from += min(head[u], H - 1) * (D * 2);
+    x[u] = u16x8{};
     if (at < p.q_pieces + p.k_pieces + p.v_pieces) x[u] = *(const u16x8 *)(from + piece * 16);
   }
 
@@ -165,6 +166,20 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
     }
   };
   turn();
+  // What a norm multiplies a head by.  Without a cache the heads' sums are made together, so that none waits for another; with one that
+  // takes registers that its rows' waves need (16396 prompt tokens to 4-bit rows and read back 106 us, one by one 100).
+  auto norm_of = [&](int u) __attribute__((always_inline)) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(widen(x[u][e]), widen(x[u][e]), s);
+    s = over_lanes<LPR>(s, [](float x, float y) { return x + y; });
+    return 1.f / sqrtf(s * (1.f / D) + p.eps);
+  };
+  float by[U];
+  if constexpr (NORM && KIND == kNoCache) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) by[u] = norm_of(u);
+  }
   bool room = false;
   int64_t at_cache = 0;
   if constexpr (KIND != kNoCache) {
@@ -202,19 +217,17 @@ __global__ void __launch_bounds__(64 * kWaves) rotate_kernel(const RotateParams 
     }
     float f = 1.f;
     if (NORM && norm) {
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(widen(x[u][e]), widen(x[u][e]), s);
-      s = over_lanes<LPR>(s, [](float x, float y) { return x + y; });
-      f = 1.f / sqrtf(s * (1.f / D) + p.eps);
+      if constexpr (KIND == kNoCache) f = by[u];
+      else f = norm_of(u);
     }
     u16x8 out;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float a = widen(x[u][e]), z = widen(y[INTERLEAVED ? e ^ 1 : e]);
+      float a = widen(x[u][e]), z = widen(y[INTERLEAVED ? e ^ 1 : e]);
+      if (NORM) a *= f, z *= f;  // (first: what the weights make of an element that is not normed yet may be past fp32's range, f then 0)
       float r = a * own[e];
       if (turned) r = fmaf(z, with[e], r);  // (elements that are not turned are not mixed with others either: 0 * inf)
-      out[e] = narrow(NORM ? r * f : r);
+      out[e] = narrow(r);
     }
     if (is_q) {
       if (valid) *(u16x8 *)(p.q_out + (row * p.q_out_stride + head[u] * D + piece * 8) * 2) = out;
