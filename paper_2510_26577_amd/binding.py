@@ -266,6 +266,24 @@ def _p(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def empty_for(stream, shape, dtype, device):
+    """A tensor that a call queued on `stream` (None: the current one) makes for its results or its scratch memory.  Another stream's comes from that
+    stream's pool, so that no work queued earlier still uses the memory, and work queued there later finds it free; and it is not handed out again
+    before what the current stream has been given by the time it is dropped: once that stream waits for `stream`, the result may be used on either."""
+    import torch
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    now = torch.cuda.current_stream(device)
+    if now.cuda_stream == stream.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(now)
+    return t
+
+
 def build_ancestor_mask_host(parent, cu_T, max_T: int):
     """numpy int32 arrays on the host -> (uint64 mask [sum_T, W], status, bad_node).  Validation variant:
     status is TVA_OK or TVA_BAD_TREE (-5), bad_node the first offending global node index or -1."""
@@ -409,9 +427,9 @@ def merge_splits(part_out, part_lse, out=None, lse=None, stream=None):
     import torch
     S, n, D = part_out.shape
     if out is None:
-        out = torch.empty((n, D), dtype=torch.float32, device=part_out.device)
+        out = empty_for(stream, (n, D), torch.float32, part_out.device)
     if lse is None:
-        lse = torch.empty((n,), dtype=torch.float32, device=part_out.device)
+        lse = empty_for(stream, (n,), torch.float32, part_out.device)
     _check(load_library().tva_merge_splits(_p(part_out), _p(part_lse), S, n, D, _p(out), _p(lse),
                                            _stream_ptr(stream)))
     return out, lse

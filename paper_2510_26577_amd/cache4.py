@@ -246,11 +246,12 @@ def plan_splits(args: Attn4Args) -> int:
     return int(n)
 
 
-def attn_workspace(args: Attn4Args, device):
-    """Makes the workspace that the block's shapes need and puts it into the block (None where none is needed)."""
+def attn_workspace(args: Attn4Args, device, stream=None):
+    """Makes the workspace that the block's shapes need and puts it into the block (None where none is needed); stream: the one that the call
+    is going to be queued on, if it is not the current one."""
     import torch
     need = workspace_bytes(args)
-    ws = torch.empty(need // 4, dtype=torch.float32, device=device) if need else None
+    ws = binding.empty_for(stream, need // 4, torch.float32, torch.device(device)) if need else None
     args.workspace, args.workspace_bytes = _p(ws), need
     args._keep = (*args._keep, ws)
     return ws
@@ -263,17 +264,17 @@ def tree_verify_attn_raw(args: Attn4Args, stream=None) -> None:
 
 def tree_verify_attn(q, k_tree, v_tree, cache: Cache, cu_T, L, *, max_T: int, max_L: int, scale: float, anc_mask=None, parent=None, out=None,
                      lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0, stream: Optional[object] = None):
-    """Tree-masked verification attention over a cache of 4-bit rows.  Returns (out bf16 [sum_T, Hq, D], lse fp32 [sum_T, Hq])."""
+    """Tree-masked verification attention over a cache of 4-bit rows.  Returns (out bf16 [sum_T, Hq, D], lse fp32 [sum_T, Hq]);
+    what is not given is made (binding.empty_for)."""
     import torch
     if out is None:
-        out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=q.device)
+        out = binding.empty_for(stream, tuple(q.shape), torch.bfloat16, q.device)
     if lse is None:
-        lse = torch.empty(tuple(q.shape[:2]), dtype=torch.float32, device=q.device)
+        lse = binding.empty_for(stream, tuple(q.shape[:2]), torch.float32, q.device)
     a = make_attn_args(q=q, k_tree=k_tree, v_tree=v_tree, cache=cache, cu_T=cu_T, L=L, max_T=max_T, max_L=max_L, scale=scale, anc_mask=anc_mask,
                        parent=parent, out=out, lse=lse, workspace=workspace, num_splits=num_splits, plan_rows=plan_rows)
     _on_gpu(q)
-    ws = attn_workspace(a, q.device) if workspace is None else None
+    if workspace is None:
+        attn_workspace(a, q.device, stream)
     tree_verify_attn_raw(a, stream)
-    if ws is not None and stream is not None:  # it goes back to the current stream's pool: not before the work on `stream` is done
-        ws.record_stream(stream)
     return out, lse

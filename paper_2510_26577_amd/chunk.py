@@ -93,11 +93,12 @@ def plan_splits(args: ChunkArgs) -> int:
     return int(n)
 
 
-def attn_workspace(args: ChunkArgs, device):
-    """Makes the workspace that the block's shapes need and puts it into the block (None where none is needed)."""
+def attn_workspace(args: ChunkArgs, device, stream=None):
+    """Makes the workspace that the block's shapes need and puts it into the block (None where none is needed); stream: the one that the call
+    is going to be queued on, if it is not the current one."""
     import torch
     need = workspace_bytes(args)
-    ws = torch.empty(need // 4, dtype=torch.float32, device=device) if need else None
+    ws = binding.empty_for(stream, need // 4, torch.float32, torch.device(device)) if need else None
     args.workspace, args.workspace_bytes = _p(ws), need
     args._keep = (*args._keep, ws)
     return ws
@@ -110,17 +111,17 @@ def attn_raw(args: ChunkArgs, stream=None) -> None:
 
 def attn(q, cache: Cache, cu_T, L, *, Hkv: int, max_T: int, max_L: int, scale: float, window: int = 0, n_first: int = 0, anc_mask=None, out=None,
          lse=None, workspace=None, num_splits: int = 0, plan_rows: int = 0, stream: Optional[object] = None):
-    """Attention of new tokens over the cache that holds them.  Returns (out bf16 [sum_T, Hq, D], lse fp32 [sum_T, Hq])."""
+    """Attention of new tokens over the cache that holds them.  Returns (out bf16 [sum_T, Hq, D], lse fp32 [sum_T, Hq]);
+    what is not given is made (binding.empty_for)."""
     import torch
     if out is None:
-        out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=q.device)
+        out = binding.empty_for(stream, tuple(q.shape), torch.bfloat16, q.device)
     if lse is None:
-        lse = torch.empty(tuple(q.shape[:2]), dtype=torch.float32, device=q.device)
+        lse = binding.empty_for(stream, tuple(q.shape[:2]), torch.float32, q.device)
     a = make_args(q=q, cache=cache, cu_T=cu_T, L=L, Hkv=Hkv, max_T=max_T, max_L=max_L, scale=scale, window=window, n_first=n_first,
                   anc_mask=anc_mask, out=out, lse=lse, workspace=workspace, num_splits=num_splits, plan_rows=plan_rows)
     _on_gpu(q)
-    ws = attn_workspace(a, q.device) if workspace is None else None
+    if workspace is None:
+        attn_workspace(a, q.device, stream)
     attn_raw(a, stream)
-    if ws is not None and stream is not None:  # it goes back to the current stream's pool: not before the work on `stream` is done
-        ws.record_stream(stream)
     return out, lse

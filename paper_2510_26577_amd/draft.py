@@ -76,16 +76,12 @@ def expand_layer(cu_N, score, logp, K: int, max_N: int, stream=None):
     import torch
     sum_N, V = int(logp.shape[0]), int(logp.shape[1])
     dev = logp.device
-    cs = torch.empty(sum_N * K, dtype=torch.float32, device=dev)
-    cp = torch.empty(sum_N * K, dtype=torch.int32, device=dev)
-    ct = torch.empty(sum_N * K, dtype=torch.int32, device=dev)
+    cs, cp, ct = (binding.empty_for(stream, sum_N * K, dtype, dev) for dtype in (torch.float32, torch.int32, torch.int32))
     need = expand_workspace_bytes(cu_N.numel() - 1, V, K, sum_N)
-    ws = torch.empty(max(1, need // 8), dtype=torch.int64, device=dev)
+    ws = binding.empty_for(stream, max(1, need // 8), torch.int64, dev)
     a = make_expand_args(cu_N=cu_N, score=score, logp=logp, K=K, sum_N=sum_N, max_N=max_N, cand_score=cs, cand_parent=cp,
                          cand_token=ct, workspace=ws, workspace_bytes=need)
     expand_layer_raw(a, stream)
-    if stream is not None:
-        ws.record_stream(stream)  # (it goes back to the current stream's pool when this returns)
     return cs, cp, ct
 
 
@@ -111,9 +107,9 @@ def breadth_count(cand_score, draft_cost_row, target_cost_one: float, C1: float,
     import torch
     B, N = int(cand_score.shape[0]), int(cand_score.shape[1])
     if count is None:
-        count = torch.empty(1, dtype=torch.int32, device=cand_score.device)
+        count = binding.empty_for(stream, 1, torch.int32, cand_score.device)
     if u_c_at is None:
-        u_c_at = torch.empty(2, dtype=torch.float64, device=cand_score.device)
+        u_c_at = binding.empty_for(stream, 2, torch.float64, cand_score.device)
     _check(_lib().tva_layer_breadth_count(_p(cand_score), B, N, _p(draft_cost_row), float(target_cost_one), float(C1),
                                           _p(count), _p(u_c_at), _p(err_flag), _stream_ptr(stream)))
     return count, u_c_at

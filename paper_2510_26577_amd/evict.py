@@ -142,9 +142,9 @@ def select(weight, L, keep, *, max_L: int, max_keep: int, n_first: int = 0, newe
     """Which slots stay: returns (src int32 [.., max_keep], L_out int32 [B]); entries of src from L_out[b] on are not written."""
     import torch
     if src is None:
-        src = torch.empty((*weight.shape[:-1], max(1, int(max_keep))), dtype=torch.int32, device=weight.device)
+        src = binding.empty_for(stream, (*weight.shape[:-1], max(1, int(max_keep))), torch.int32, weight.device)
     if L_out is None:
-        L_out = torch.empty(int(weight.shape[-3]), dtype=torch.int32, device=weight.device)
+        L_out = binding.empty_for(stream, int(weight.shape[-3]), torch.int32, weight.device)
     args = make_select_args(weight=weight, L=L, keep=keep, max_L=max_L, src=src, L_out=L_out, n_first=n_first, newest=newest, pos=pos)
     _on_gpu(weight)
     select_raw(args, stream)

@@ -155,12 +155,11 @@ def append_raw(args: AppendArgs, stream=None) -> None:
 
 
 def rotate(*, stream=None, q=None, k=None, q_out=None, k_out=None, **kw):
-    """Keyword arguments of make_rotate_args; outputs that are not given are made.  Returns (q_out, k_out)."""
-    import torch
+    """Keyword arguments of make_rotate_args; outputs that are not given are made (binding.empty_for).  Returns (q_out, k_out)."""
     if q is not None and q_out is None:
-        q_out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+        q_out = binding.empty_for(stream, tuple(q.shape), q.dtype, q.device)
     if k is not None and k_out is None:
-        k_out = torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device)
+        k_out = binding.empty_for(stream, tuple(k.shape), k.dtype, k.device)
     args = make_rotate_args(q=q, k=k, q_out=q_out, k_out=k_out, **kw)
     _on_gpu(q if q is not None else k)
     rotate_raw(args, stream)
@@ -168,10 +167,10 @@ def rotate(*, stream=None, q=None, k=None, q_out=None, k_out=None, **kw):
 
 
 def append(*, stream=None, q=None, q_out=None, **kw):
-    """Keyword arguments of make_append_args; the cache is written in place.  Returns q_out (made where q is given without)."""
-    import torch
+    """Keyword arguments of make_append_args; the cache is written in place.  Returns q_out (made where q is given without:
+    binding.empty_for)."""
     if q is not None and q_out is None:
-        q_out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+        q_out = binding.empty_for(stream, tuple(q.shape), q.dtype, q.device)
     args = make_append_args(q=q, q_out=q_out, **kw)
     _on_gpu(kw["k"])
     append_raw(args, stream)
