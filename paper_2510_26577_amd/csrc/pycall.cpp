@@ -102,18 +102,35 @@ void strides_of(PyObject *o, int64_t *page, int64_t *tok, int64_t *head) {
   PyObject **v = PySequence_Fast_ITEMS(seq.get());
   *page = integer(v[0]), *tok = integer(v[1]), *head = integer(v[2]);
 }
-at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &like) {
-  at::AutoDispatchBelowADInplaceOrView below;
-  return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
-}
-// Scratch memory made here comes from the current stream's pool and goes back to it when the call returns.  Work queued
-// on another stream still uses it then: the allocator is told, and hands it out again only behind that work.
-void hold_for(const at::Tensor &scratch, void *st, PyObject *stream_given) {
-  if (!scratch.defined() || stream_given == Py_None) return;
-  const auto device = scratch.device().index();
-  if (c10::hip::getCurrentHIPStream(device).stream() == st) return;
-  c10::hip::HIPCachingAllocator::recordStream(scratch.storage().data_ptr(), c10::hip::getStreamFromExternal(static_cast<hipStream_t>(st), device));
-}
+// Where a call's work goes, and where what it makes for that comes from: the current stream's memory, or, queued on another stream, that stream's,
+// so that no work queued earlier still uses it and work queued there later finds it free.  Results are held for the current stream too: it may
+// read them (once it waits for the call's) before they are dropped.
+struct Queue {
+  void *st;
+  bool other = false;
+  c10::DeviceIndex device = -1;
+  Queue(PyObject *o, const at::Tensor &like) : st(stream_of(o)) {
+    if (o == Py_None || !like.is_cuda()) return;
+    device = like.device().index();
+    other = c10::hip::getCurrentHIPStream(device).stream() != st;
+  }
+  at::Tensor scratch(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &like) const {
+    at::AutoDispatchBelowADInplaceOrView below;
+    const auto options = at::TensorOptions().dtype(type).device(like.device());
+    if (!other) return at::empty(sizes, options);
+    struct Back {
+      c10::hip::HIPStream stream;
+      ~Back() { c10::hip::setCurrentHIPStream(stream); }
+    } back{c10::hip::getCurrentHIPStream(device)};
+    c10::hip::setCurrentHIPStream(c10::hip::getStreamFromExternal(static_cast<hipStream_t>(st), device));
+    return at::empty(sizes, options);
+  }
+  at::Tensor result(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &like) const {
+    at::Tensor t = scratch(sizes, type, like);
+    if (other) c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), c10::hip::getCurrentHIPStream(device));
+    return t;
+  }
+};
 int64_t bytes_of(const at::Tensor &t) { return t.numel() * static_cast<int64_t>(t.element_size()); }
 
 // the library's call without the interpreter's lock (as ctypes makes it)
@@ -200,16 +217,15 @@ PyObject *attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const HostInts lengths(a[29], t.B);
   t.L_host = lengths.data;
   at::Tensor new_out, new_lse, new_ws;
-  if (!out) new_out = make(q.sizes(), at::kFloat, q), out = &new_out;
-  if (!lse) new_lse = make({q.size(0), q.size(1)}, at::kFloat, q), lse = &new_lse;
+  const Queue to(a[19], q);
+  if (!out) new_out = to.result(q.sizes(), at::kFloat, q), out = &new_out;
+  if (!lse) new_lse = to.result({q.size(0), q.size(1)}, at::kFloat, q), lse = &new_lse;
   t.out = ptr<float>(out), t.lse = ptr<float>(lse);
   const size_t need = lib.workspace_bytes(&t);
   if (need == (size_t)-1) return PyLong_FromLong(TVA_INVALID_ARG);
-  if (need > 0 && (!ws || (size_t)bytes_of(*ws) < need)) new_ws = make({(int64_t)((need + 3) / 4)}, at::kFloat, q), ws = &new_ws;
+  if (need > 0 && (!ws || (size_t)bytes_of(*ws) < need)) new_ws = to.scratch({(int64_t)((need + 3) / 4)}, at::kFloat, q), ws = &new_ws;
   if (ws) t.workspace = ws->data_ptr(), t.workspace_bytes = (size_t)bytes_of(*ws);
-  void *st = stream_of(a[19]);
-  const int rc = unlocked([&] { return lib.attn(&t, st); });
-  hold_for(new_ws, st, a[19]);
+  const int rc = unlocked([&] { return lib.attn(&t, to.st); });
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return pair(*out, *lse);
   END_HANDLE_TH_ERRORS
@@ -224,11 +240,11 @@ PyObject *ancestor_mask(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const int32_t max_T = int32(a[2]);
   const int32_t W = mask ? static_cast<int32_t>(mask->size(1)) : max_T > 64 ? (max_T + 63) / 64 : 1;
   at::Tensor made;
-  if (!mask) made = make({parent.numel(), W}, at::kLong, parent), mask = &made;
-  void *st = stream_of(a[5]);
+  const Queue to(a[5], parent);
+  if (!mask) made = to.result({parent.numel(), W}, at::kLong, parent), mask = &made;
   const int rc = unlocked([&] {
     return lib.mask(ptr<const int32_t>(&parent), ptr<const int32_t>(&cu_T), static_cast<int32_t>(cu_T.numel() - 1), max_T, W,
-                    ptr<uint64_t>(mask), ptr<int32_t>(flag), st);
+                    ptr<uint64_t>(mask), ptr<int32_t>(flag), to.st);
   });
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return THPVariable_Wrap(*mask);
@@ -244,14 +260,14 @@ PyObject *accept_greedy(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const int64_t B = cu_T.numel() - 1, max_path = integer(a[4]);
   at::Tensor new_path, new_len, new_next;
   const bool fill = !path;  // (a path made here has -1 behind the accepted nodes)
-  if (!path) new_path = make({B, max_path}, at::kInt, cu_T), path = &new_path;
-  if (!len) new_len = make({B}, at::kInt, cu_T), len = &new_len;
-  if (!next) new_next = make({B}, at::kInt, cu_T), next = &new_next;
-  void *st = stream_of(a[8]);
+  const Queue to(a[8], cu_T);
+  if (!path) new_path = to.result({B, max_path}, at::kInt, cu_T), path = &new_path;
+  if (!len) new_len = to.result({B}, at::kInt, cu_T), len = &new_len;
+  if (!next) new_next = to.result({B}, at::kInt, cu_T), next = &new_next;
   const int rc = unlocked([&] {
     return (fill ? lib.greedy_filled : lib.greedy)(ptr<const int32_t>(&parent), ptr<const int32_t>(&cu_T), ptr<const int32_t>(&draft),
                                                    ptr<const int32_t>(&target), (int32_t)B, (int32_t)max_path, ptr<int32_t>(path),
-                                                   ptr<int32_t>(len), ptr<int32_t>(next), st);
+                                                   ptr<int32_t>(len), ptr<int32_t>(next), to.st);
   });
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return triple(*path, *len, *next);
@@ -269,11 +285,12 @@ PyObject *accept_sampling(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const int64_t B = cu_T.numel() - 1, V = p.size(1), max_path = integer(a[7]);
   t.B = (int32_t)B, t.V = (int32_t)V, t.max_path = (int32_t)max_path;
   t.workgroups_per_sequence = int32(a[13]), t.sum_T = int32(a[14]), t.unit_rows = truth(a[15]);
-  at::Tensor path = make({B, max_path}, at::kInt, cu_T), len = make({B}, at::kInt, cu_T), next = make({B}, at::kInt, cu_T), made, made_ws;
-  if (!residual) made = make({B > 1 ? B : 1, V}, at::kFloat, cu_T), residual = &made;
+  const Queue to(a[10], cu_T);
+  at::Tensor path = to.result({B, max_path}, at::kInt, cu_T), len = to.result({B}, at::kInt, cu_T), next = to.result({B}, at::kInt, cu_T), made, made_ws;
+  if (!residual) made = to.scratch({B > 1 ? B : 1, V}, at::kFloat, cu_T), residual = &made;
   if (!ws && truth(a[12])) {
     const size_t need = lib.sample_workspace(t.B, t.sum_T, t.V) / 8;
-    made_ws = make({(int64_t)(need > 1 ? need : 1)}, at::kLong, cu_T), ws = &made_ws;
+    made_ws = to.scratch({(int64_t)(need > 1 ? need : 1)}, at::kLong, cu_T), ws = &made_ws;
   }
   t.parent = ptr<const int32_t>(tensor_or_null(a[0])), t.cu_T = ptr<const int32_t>(&cu_T);
   t.draft_token = ptr<const int32_t>(tensor_or_null(a[2]));
@@ -282,10 +299,7 @@ PyObject *accept_sampling(PyObject *, PyObject *const *a, Py_ssize_t n) {
   t.residual = ptr<float>(residual), t.err_flag = ptr<int32_t>(tensor_or_null(a[9]));
   t.path = ptr<int32_t>(&path), t.path_len = ptr<int32_t>(&len), t.next_token = ptr<int32_t>(&next);
   if (ws) t.workspace = ws->data_ptr(), t.workspace_bytes = (size_t)bytes_of(*ws);
-  void *st = stream_of(a[10]);
-  const int rc = unlocked([&] { return lib.sampling_filled(&t, st); });
-  hold_for(made, st, a[10]);
-  hold_for(made_ws, st, a[10]);
+  const int rc = unlocked([&] { return lib.sampling_filled(&t, to.st); });
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return triple(path, len, next);
   END_HANDLE_TH_ERRORS
@@ -329,19 +343,18 @@ PyObject *rerank_count(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const int32_t B = (int32_t)scores.size(0), N = (int32_t)scores.size(1), m = int32(a[2]);
   const double C3 = number(a[3]);
   at::Tensor new_count, new_cu, new_ws;
-  if (!count) new_count = make({1}, at::kInt, scores), count = &new_count;
-  if (!cu_T) new_cu = make({B + 1}, at::kInt, scores), cu_T = &new_cu;
+  const Queue to(a[7], scores);
+  if (!count) new_count = to.result({1}, at::kInt, scores), count = &new_count;
+  if (!cu_T) new_cu = to.result({B + 1}, at::kInt, scores), cu_T = &new_cu;
   if (!ws) {
     const size_t need = lib.rerank_workspace(B, N, m);
     if (need == (size_t)-1) return PyLong_FromLong(TVA_INVALID_ARG);
-    new_ws = make({(int64_t)(need / 4 > 1 ? need / 4 : 1)}, at::kFloat, scores), ws = &new_ws;
+    new_ws = to.scratch({(int64_t)(need / 4 > 1 ? need / 4 : 1)}, at::kFloat, scores), ws = &new_ws;
   }
-  void *st = stream_of(a[7]);
   const int rc = unlocked([&] {
     return lib.rerank(ptr<const float>(&scores), B, N, ptr<const double>(&cost), m, C3, ptr<int32_t>(count), ptr<int32_t>(cu_T),
-                      ptr<int32_t>(flag), ws->data_ptr(), (size_t)bytes_of(*ws), st);
+                      ptr<int32_t>(flag), ws->data_ptr(), (size_t)bytes_of(*ws), to.st);
   });
-  hold_for(new_ws, st, a[7]);
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return pair(*count, *cu_T);
   END_HANDLE_TH_ERRORS
@@ -354,16 +367,16 @@ PyObject *select_subtree(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const at::Tensor &score = tensor(a[0]), &parent = tensor(a[1]), &cu_M = tensor(a[2]), &cu_T = tensor(a[3]);
   const at::Tensor *old_index = tensor_or_null(a[5]), *new_parent = tensor_or_null(a[6]), *flag = tensor_or_null(a[7]);
   at::Tensor new_old, new_new;
+  const Queue to(a[8], score);
   if (!old_index || !new_parent) {
     const int64_t kept = integer(a[9]) > 1 ? integer(a[9]) : 1;
-    if (!old_index) new_old = make({kept}, at::kInt, score), old_index = &new_old;
-    if (!new_parent) new_new = make({kept}, at::kInt, score), new_parent = &new_new;
+    if (!old_index) new_old = to.result({kept}, at::kInt, score), old_index = &new_old;
+    if (!new_parent) new_new = to.result({kept}, at::kInt, score), new_parent = &new_new;
   }
   const int32_t max_M = int32(a[4]);
-  void *st = stream_of(a[8]);
   const int rc = unlocked([&] {
     return lib.subtree(ptr<const float>(&score), ptr<const int32_t>(&parent), ptr<const int32_t>(&cu_M), ptr<const int32_t>(&cu_T),
-                       (int32_t)(cu_M.numel() - 1), max_M, ptr<int32_t>(old_index), ptr<int32_t>(new_parent), ptr<int32_t>(flag), st);
+                       (int32_t)(cu_M.numel() - 1), max_M, ptr<int32_t>(old_index), ptr<int32_t>(new_parent), ptr<int32_t>(flag), to.st);
   });
   if (rc != TVA_OK) return PyLong_FromLong(rc);
   return pair(*old_index, *new_parent);

@@ -18,13 +18,14 @@ def torch():
 
 def _calls(torch):
     """name -> a call on tensors that live on, given its stream; its results."""
-    from paper_2510_26577_amd import binding, cache4, chunk, draft, evict, rotary
+    from paper_2510_26577_amd import binding, cache4, chunk, draft, evict, rotary, verify, workloads as wl
     Hq, Hkv, D, n = 8, 2, 64, 40
     x = torch.randn((n, Hq + 2 * Hkv, D), device="cuda").bfloat16()
     q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
     freq, cu, zero = cc.dev(rotary.frequencies(D)[0]), cc.dev([0, n], np.int32), cc.dev([0], np.int32)
     rows = [torch.zeros((600, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
-    cache = cache4.make_cache(kind=0, k=rows[0], v=rows[1], cu_L=cc.dev([0, 600], np.int32))
+    room = cc.dev([0, 600], np.int32)
+    cache = cache4.make_cache(kind=0, k=rows[0], v=rows[1], cu_L=room)
     four = cache4.make_cache(kind=2, k=torch.zeros((600, Hkv, D // 2), dtype=torch.uint8, device="cuda"), v=torch.zeros((600, Hkv, D // 2), dtype=torch.uint8, device="cuda"),
                              k_row_scale=torch.full((600 * Hkv, D // 32), 120, dtype=torch.uint8, device="cuda"),
                              v_row_scale=torch.ones(600 * Hkv, dtype=torch.bfloat16, device="cuda"), cu_L=cc.dev([0, 600], np.int32))
@@ -37,7 +38,20 @@ def _calls(torch):
     score, logp = torch.zeros(5, device="cuda"), torch.log_softmax(torch.randn((5, 2000), device="cuda"), -1)
     chance = torch.sort(torch.rand((2, 100), device="cuda"), descending=True)[0]
     cost = torch.cumsum(torch.full((100,), 0.05, dtype=torch.float64, device="cuda"), 0) + 1.0
+    rng = np.random.Generator(np.random.PCG64(31))
+    tree, count = wl.tree_expand_prune(rng, n).astype(np.int32), np.array([0, n], np.int32)
+    p, r, tok, u, uf = wl.sampling_inputs(rng, tree, count, 20000, drift=0.6)
+    parent, tokens = cc.dev(tree), cc.dev(tok, np.int32)
+    sample = [parent, cu, tokens, *(cc.dev(x, np.float32) for x in (p, r, u, uf))]
+    scores, heads = torch.rand((16, 145), device="cuda"), cc.dev([0, n // 2], np.int32)
+    node_score = torch.sort(torch.rand(n, device="cuda"), descending=True)[0]
     return {
+        "verify": lambda s: binding.tree_verify_attn(*packed, *rows, None, cu, L, max_T=n, max_L=500, scale=0.1, cu_L=room, parent=parent, num_splits=8, stream=s),
+        "masks": lambda s: (binding.build_ancestor_mask(parent, cu, n, stream=s),),
+        "greedy": lambda s: verify.accept_greedy(parent, cu, tokens, tokens, 9, stream=s),
+        "sampling": lambda s: verify.accept_sampling(*sample, 9, stream=s),
+        "rerank": lambda s: draft.rerank_count(scores, cost, 72, 1.0, stream=s),
+        "subtree": lambda s: draft.select_subtree(node_score, parent, cu, heads, n, total_kept=n // 2, stream=s),
         "rotate": lambda s: rotary.rotate(q=q, k=k, stream=s, **place),
         "append": lambda s: (rotary.append(q=q, k=k, v=v, cache=cache, stream=s, **place),),
         "attn": lambda s: chunk.attn(packed[0], cache, cu, L, Hkv=Hkv, max_T=n, max_L=500, scale=0.1, num_splits=3, stream=s),
@@ -54,7 +68,7 @@ def calls(torch):
     return _calls(torch)
 
 
-NAMES = ["rotate", "append", "attn", "attn 4 bit", "select", "merge", "expand", "breadth"]
+NAMES = ["verify", "masks", "greedy", "sampling", "rerank", "subtree", "rotate", "append", "attn", "attn 4 bit", "select", "merge", "expand", "breadth"]
 
 
 def _same(a, b):
