@@ -45,7 +45,7 @@ int tva_rotary_frequencies(int32_t scaling, int32_t dims, double base, double fa
  * Angles are reduced in 64 bits (any int32 position), sums and products are fp32, the result is rounded to bf16 once.  (A
  * norm's sum of squares is an fp32 number: from 2^128 on it is infinite, and the head becomes 0, but for elements that are infinite
  * themselves; with eps 0 a head whose squares all vanish in it has no finite norm.)
- * Rows from cu_T[B] on are left as they are.  q_out may be q with the same stride, k_out k (in place); other
+ * Rows before cu_T[0] and from cu_T[B] on are left as they are.  q_out may be q with the same stride, k_out k (in place); other
  * overlaps are not allowed.  q or k may be NULL (then so is its output).
  */
 typedef struct tva_rotate_args {
@@ -102,8 +102,8 @@ size_t tva_sizeof_append_args(void);
  *     lse = log sum exp(scale * <q, K>),  out = sum exp(scale * <q, K> - lse) V     over the keys that are seen
  * out is bf16, rounded once from fp32; lse fp32, natural logarithm, may be NULL.  Sums and softmax weights are fp32; as a factor of V
  * a weight is rounded to bf16 (half a step, 2^-8 of it at most), with plan_rows 32 to 16 bits.  A row that sees nothing gets out = 0,
- * lse = -inf.  A key or value that is not finite reaches the rows that see it, and no others.  Rows from cu_T[B] on are left as they
- * are.  Positions outside the sequence's room are not read; a page none of whose positions any token sees may have an entry below 0 in
+ * lse = -inf.  A key or value that is not finite reaches the rows that see it, and no others.  Rows before cu_T[0] and from cu_T[B]
+ * on are left as they are.  Positions outside the sequence's room are not read; a page none of whose positions any token sees may have an entry below 0 in
  * the page table (given back: page 0 is read in its place, to no effect), others below L[b] + T_b are pages.  E2M1 caches are read by
  * tva_tree_verify_attn_4bit: TVA_UNSUPPORTED here.
  * max_T and max_L size the launch: rows i >= max_T are not computed; max_L only shapes the plan.

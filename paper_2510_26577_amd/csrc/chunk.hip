@@ -93,6 +93,7 @@ struct Block {
       auto first = [&](int n, int row) __attribute__((always_inline)) { return (int64_t)row * p.G / R + n; };
       const sequences::Place place = sequences::find(p.cu_T, p.L, p.B, number, first);
       b = same(place.b), t0 = same(place.t0), T = place.t1 - place.t0, L = place.L, from = first(b, t0);
+      if (number < from) T = 0, from = number;  // in front of the first sequence (cu_T[0] > 0): no rows
     }
     T = same(min(T, p.max_T)), L = same(max(L, 0));
     const int64_t at = (number - from) * R, all = (int64_t)T * p.G;
