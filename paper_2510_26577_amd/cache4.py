@@ -108,6 +108,14 @@ def _on_gpu(t) -> None:
         raise ValueError(f"tensors lie on {t.device}, not on a GPU")
 
 
+def _on_current_gpu(t) -> None:
+    """The work is queued on the current device: another one's memory is not its own."""
+    import torch
+    _on_gpu(t)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors lie on {t.device}, the current GPU is cuda:{torch.cuda.current_device()}")
+
+
 def _fits(cache, B: int, *tensors) -> None:
     """The sequences' places are there, and everything lies on one device (of a cache made here; a copy is not looked into)."""
     k = getattr(cache, "_keep", ())

@@ -8,7 +8,7 @@ from typing import Optional
 
 from . import binding
 from .binding import _p
-from .cache4 import Cache, _at_least, _fits, _indices, _on_gpu, _typed
+from .cache4 import Cache, _at_least, _fits, _indices, _on_current_gpu, _typed
 from .rotary import _heads
 
 _ready = False
@@ -120,7 +120,7 @@ def attn(q, cache: Cache, cu_T, L, *, Hkv: int, max_T: int, max_L: int, scale: f
         lse = binding.empty_for(stream, tuple(q.shape[:2]), torch.float32, q.device)
     a = make_args(q=q, cache=cache, cu_T=cu_T, L=L, Hkv=Hkv, max_T=max_T, max_L=max_L, scale=scale, window=window, n_first=n_first,
                   anc_mask=anc_mask, out=out, lse=lse, workspace=workspace, num_splits=num_splits, plan_rows=plan_rows)
-    _on_gpu(q)
+    _on_current_gpu(q)
     if workspace is None:
         attn_workspace(a, q.device, stream)
     attn_raw(a, stream)

@@ -7,7 +7,7 @@ import ctypes
 
 from . import binding
 from .binding import _p
-from .cache4 import Cache, _at_least, _fits, _indices, _is, _on_gpu, _one_device, _typed
+from .cache4 import Cache, _at_least, _fits, _indices, _is, _on_current_gpu, _one_device, _typed
 
 PLAIN, LINEAR, BASE, WAVELENGTH, RAMP = range(5)  # tva_rotary_scaling
 
@@ -161,7 +161,7 @@ def rotate(*, stream=None, q=None, k=None, q_out=None, k_out=None, **kw):
     if k is not None and k_out is None:
         k_out = binding.empty_for(stream, tuple(k.shape), k.dtype, k.device)
     args = make_rotate_args(q=q, k=k, q_out=q_out, k_out=k_out, **kw)
-    _on_gpu(q if q is not None else k)
+    _on_current_gpu(q if q is not None else k)
     rotate_raw(args, stream)
     return q_out, k_out
 
@@ -172,6 +172,6 @@ def append(*, stream=None, q=None, q_out=None, **kw):
     if q is not None and q_out is None:
         q_out = binding.empty_for(stream, tuple(q.shape), q.dtype, q.device)
     args = make_append_args(q=q, q_out=q_out, **kw)
-    _on_gpu(kw["k"])
+    _on_current_gpu(kw["k"])
     append_raw(args, stream)
     return q_out
