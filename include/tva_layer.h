@@ -96,16 +96,18 @@ size_t tva_sizeof_append_args(void);
  * T_b = cu_T[b+1]-cu_T[b] of them, any number; L[b] >= 0 cached tokens before them.
  *   without anc_mask  a chunk: token i has position P = L[b] + i and sees the new tokens j <= i
  *   with anc_mask     a draft tree: node i has position P = L[b] + (bits set in its row) - 1 and sees the nodes j whose bit is
- *                     set (T_b <= TVA_MAX_TREE)
+ *                     set (T_b <= TVA_MAX_TREE, bits from T_b on are 0)
  * and of the cached tokens all.  With window > 0 a token at position P sees, of those, only keys whose own position is above
  * P - window, or below n_first (window 1: itself and the first ones).  Query head h reads KV head h / (Hq/Hkv).
  *     lse = log sum exp(scale * <q, K>),  out = sum exp(scale * <q, K> - lse) V     over the keys that are seen
  * out is bf16, rounded once from fp32; lse fp32, natural logarithm, may be NULL.  Sums and softmax weights are fp32; as a factor of V
- * a weight is rounded to bf16 (half a step, 2^-8 of it at most), with plan_rows 32 to 16 bits.  A row that sees nothing gets out = 0,
- * lse = -inf.  A key or value that is not finite reaches the rows that see it, and no others.  Rows before cu_T[0] and from cu_T[B]
- * on are left as they are.  Positions outside the sequence's room are not read; a page none of whose positions any token sees may have an entry below 0 in
- * the page table (given back: page 0 is read in its place, to no effect), others below L[b] + T_b are pages.  E2M1 caches are read by
- * tva_tree_verify_attn_4bit: TVA_UNSUPPORTED here.
+ * a weight is rounded to bf16 (half a step, 2^-8 of it at most), with plan_rows 32 to 16 bits.  Where the library chooses the rows
+ * (plan_rows 0), which of the two a row gets therefore goes by the shapes of the call; batches of single tokens with up to 32 query
+ * heads to a KV head get 32 rows, and plan_rows 32 gives them to any call.
+ * A row that sees nothing gets out = 0, lse = -inf.  A key or value that is not finite reaches the rows that see it, and no others.
+ * Rows before cu_T[0] and from cu_T[B] on are left as they are.  Positions outside the sequence's room are not read; a page none of
+ * whose positions any token sees may have an entry below 0 in the page table (given back: page 0 is read in its place, to no effect),
+ * others below L[b] + T_b are pages.  E2M1 caches are read by tva_tree_verify_attn_4bit: TVA_UNSUPPORTED here.
  * max_T and max_L size the launch: rows i >= max_T are not computed; max_L only shapes the plan.
  * The workspace holds partial results where keys are split (0 bytes when nothing is); what it holds before does not matter, and
  * calls that overlap need one each.  There are 65535 row blocks at most, sum_T * Hq / Hkv / (rows per workgroup) + B (TVA_UNSUPPORTED).

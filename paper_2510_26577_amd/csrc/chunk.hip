@@ -12,8 +12,8 @@
 // 128 and 256 rows are bound by the instructions of a tile: all waves bring 64-key tiles to LDS together (through registers, K two tiles ahead;
 // 8-bit rows are widened on the way) and read their operands there, K as rows, V by transposing reads.  2048 tokens behind 30000: 965 us,
 // 1.08 PFLOP/s (a library product of 8192^3: 1.26 to 1.36); per matrix instruction, which takes the matrix unit 32 cycles, 5.6 vector
-// instructions and an exponential among them take the vector unit 34, of which it can do 16 under the matrix instruction; the matrix units are
-// busy for 51 % of the cycles, and the chip lowers its clock to 1.7 to 2.0 GHz under that load.  128 rows leave two workgroups to a compute
+// instructions, an exponential among them, take the vector unit 34; counters have the matrix units busy for 51 % of the cycles, and the chip
+// lowers its clock to 1.7 to 2.0 GHz under that load.  128 rows leave two workgroups to a compute
 // unit, which fill each other's barriers and share long and short blocks; 256 bring every tile half as often.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -60,7 +60,8 @@ __device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstla
 // A row block of one sequence: where its rows and its keys lie.
 // Blocks are numbered in one of three ways, of which the launch takes one:
 //   by their keys  up to 64 sequences: those with the most keys first, and of each its last block, which sees the most, first.  A lane per
-//                  sequence finds where its blocks begin.  (16 sequences of 1 to 333 tokens behind 100 to 8000, 8-bit rows: 201 us, by rows 259)
+//                  sequence finds where its blocks begin.  (16 sequences of 1 to 333 tokens behind 100 to 8000, 8-bit rows, one set of such
+//                  lengths: 201 us, by rows 259; six other sets 203 to 265)
 //   evenly         `each` for every sequence
 //   by rows        a sequence's first is floor(cu_T[b] G / rows) + b: one of n rows has ceil(n / rows) of the numbers up to the next one's first,
 //                  which are at least that many
@@ -739,8 +740,8 @@ struct ChunkPlan {
 // behind 1500 22.4 and 20.2, 60 behind 4096 25.7 and 23.3).  256 rows, which bring half as many tiles as 128, where 128 rows have twice the
 // blocks, their keys are about as many and there are workgroups for every compute unit (2048 tokens behind 30000: 948 us, with 128 rows 1058;
 // 8192 in a window of 4096 525 and 560) or 128 rows would have long parts (512 behind 16384 147 us, with 128 rows 161; 32 times 60 nodes behind
-// 4096 166 and 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90, 16 ragged ones of 1 to 333 behind 100 to 8000 223 and
-// 201, 70 of 1 to 30 behind up to 300 46 and 30), or where there are several rounds of blocks with many keys (4096 tokens 150 and 165; 10 times
+// 4096 166 and 185; but 60 behind 8192 32 and 29, 8 ragged ones of 10 to 100 119 and 90, one set of 16 ragged ones of 1 to 333 behind 100 to
+// 8000 223 and 201, 70 of 1 to 30 behind up to 300 46 and 30), or where there are several rounds of blocks with many keys (4096 tokens 150 and 165; 10 times
 // 2048 440 and 465; but 20 times 512 108 and 97, 70 ragged ones of 1 to 120 behind up to 3000 252 and 215).  A prompt's first chunk has row
 // blocks of one tile to all, which two 128-row workgroups per CU level out (2048 tokens: 54 us, with 256 rows 63).  (A batch whose longest
 // sequence is alone with its length waits for it: max_L says no more.)

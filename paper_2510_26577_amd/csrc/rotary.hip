@@ -7,7 +7,8 @@
 // wave-wide piece in one dimension: with tokens and pieces apart waves start in another order (62 us in the place of 56).
 //   8204 tokens of 64 + 8 heads of 128, half of each turned, interleaved, 288 MB   55 us  5.2 TB/s (a copy: 5.1)
 //   16384 tokens of 32 + 8 heads of 128, normed, 336 MB                            68 us  4.9 TB/s
-//   16396 of 32 + 8 + 8, normed, K and V to 4-bit rows, 352 MB                     87 us  4.0 TB/s (1.26 times the vector instructions)
+//   16396 of 32 + 8 + 8, normed, K and V to 4-bit rows, 352 MB                     85 us  4.1 TB/s (1.25 times the vector instructions)
+//   the same not normed and to 16-bit rows, 384 MB, 75 us, to 8-bit rows, 352 MB, 73
 // Small calls (a tree's nodes, 64 tokens) are one launch of 4.6 to 5.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
