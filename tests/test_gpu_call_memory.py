@@ -148,3 +148,28 @@ def test_results_that_are_dropped_behind_their_use_are_not_written_before_it(tor
     assert not places & _places(again)
     torch.cuda.synchronize()
     assert _same(used, want) and _same(again, want)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_calls_on_a_second_stream_of_a_capture(torch, calls, name):
+    """Queued on a stream that forks off the captured one: replays, with eager calls and other memory between them, give the eager result."""
+    want = [t.clone() for t in calls[name](None)]
+    s, fork, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        fork.wait_stream(s)
+        got = calls[name](fork)
+        s.wait_stream(fork)
+        more = [torch.zeros_like(t) for t in got]  # (would take memory that the call has let go)
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        other = _like(got)
+        for t in other:
+            t.fill_(255)
+        eager = calls[name](None)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(got, want) and _same(eager, want) and not any(bool(t.any()) for t in more)
+        del other, eager
